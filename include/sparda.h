@@ -30,6 +30,13 @@
  *   sparda_indexer_kl       Q, K, F, K~ -> the indexer-training loss and its gradient w.r.t. F
  *                           (Sec. 4.2, Eq. 6-7)
  *
+ * and, for checking a tree of drafted tokens in one step instead of decoding one token:
+ *
+ *   sparda_tree_select      F, K~ -> block sets of every node, sequences of different lengths
+ *   sparda_tree_attn        Q, K, V, sets, drafted K and V -> O: the blocks and the node's ancestors
+ *   sparda_tree_verify      probabilities, random numbers -> the accepted path and the next token
+ *   sparda_tree_commit      the accepted path's K and V -> the caches of all layers, and K~
+ *
  * Conventions shared by every call:
  *   - Every function returns an int status: SPARDA_OK (0) or a negative SPARDA_ERR_* code.  No
  *     call throws, aborts or prints.  sparda_last_error_detail() gives a human-readable reason
@@ -100,7 +107,9 @@ enum sparda_op {
   SPARDA_OP_SPARSE_ATTN = 2,
   SPARDA_OP_MULTIHEAD_SELECT = 3,
   SPARDA_OP_INDEXER_KL = 4,
-  SPARDA_OP_DECODE_STEP = 5
+  SPARDA_OP_DECODE_STEP = 5,
+  SPARDA_OP_TREE_SELECT = 6, /* n_q = n_nodes, q_pos0 = t_max */
+  SPARDA_OP_TREE_ATTN = 7    /* n_q = n_nodes, q_pos0 = t_max */
 };
 
 /*
@@ -368,6 +377,121 @@ int sparda_stage_append_kv(const sparda_shape* shape, const void* k_new, const v
  */
 int sparda_writeback_kv(const sparda_shape* shape, const void* k_new, const void* v_new, int32_t n_new, int64_t pos0,
                         void* host_k, void* host_v, int32_t n_workgroups, hipStream_t stream);
+
+/*
+ * ---- Trees of drafted tokens -----------------------------------------------------------------
+ *
+ * A decode step yields one token per sequence.  With tokens drafted ahead (by a small model, or
+ * several heads), one step checks a whole tree of them: select, attend, verify, commit.
+ *   n_nodes    : nodes per sequence, 1 .. 64 (SPARDA_ERR_UNSUPPORTED above).  Node 0 is the last
+ *                sampled token, whose K and V are not in the caches yet; the others are drafted.
+ *   parent  in : int32 [B][n_nodes] device.  parent[0] = -1 and 0 <= parent[i] < i: a chain has
+ *                parent[i] = i - 1.  Any other value marks an absent node (the padding of a smaller
+ *                tree), and so does an absent parent.  A(i) is node i with its ancestors.
+ *   t_ctx   in : int32 [B] device, the tokens of each sequence that its caches hold (after a
+ *                verification the sequences of a batch differ in length); negative: an absent
+ *                sequence.  Node i is at position t_ctx + |A(i)| - 1.
+ *   t_max      : no t_ctx is larger (one that is counts as t_max); it sizes the workspaces.
+ *                t_max >= 0, t_max + n_nodes <= t_cap.
+ * All four may be captured into a graph: lengths, trees and paths are read on the device.
+ */
+
+/*
+ * sparda_tree_select -- the attended block set of every node (Sec. 4.1, Eq. 4; Eq. 1), as
+ * sparda_forecast_select gives it for a row at the node's position.
+ *   f      in  : bf16 [B][Hkv][n_nodes][D] device, the nodes' Forecast rows.
+ *   k_cmp  in  : bf16 [B][Hkv][nc_cap][D] device; every window complete within a sequence's t_ctx
+ *                tokens must be valid; the last one that can be scored must be < nc_cap.
+ *   sel    out : int16 [B][Hkv][n_nodes][k_total] device: ascending block indices, -1 padded.
+ *   cnt    out : int16 [B][Hkv][n_nodes] device; 0 (and all -1) for an absent node or sequence.
+ *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_TREE_SELECT).
+ * A window counts when it is complete within t_ctx tokens: those that only drafted tokens complete
+ * have no key.  With n_local >= 2 every candidate block lies within t_ctx (a path has at most 64
+ * tokens), so the sets are those of a decode at the node's position, except where a window of the
+ * (32, 16) grid straddles the end of t_ctx; n_local = 1 returns SPARDA_ERR_UNSUPPORTED.
+ */
+int sparda_tree_select(const sparda_shape* shape, const void* f, int32_t n_nodes, const int32_t* t_ctx, int64_t t_max,
+                       const int32_t* parent, const void* k_cmp, int16_t* sel, int16_t* cnt, void* ws,
+                       size_t ws_bytes, hipStream_t stream);
+
+/*
+ * sparda_tree_attn -- attention of every node over the tokens of its blocks that the cache holds
+ * and over its own path (Sec. 4.1, Eq. 5 over the set of Eq. 1).
+ *   q      in  : bf16 [B][Hq][n_nodes][D] device.
+ *   k, v   in  : bf16 [B][Hkv][t_cap][D] device, the caches; only tokens < t_ctx are attended.
+ *   k_tree, v_tree in: bf16 [B][Hkv][n_nodes][D] device, the nodes' own K and V.
+ *   n_sel      : 1: one list for all nodes of a (batch, group), or n_nodes: one for each node.
+ *   sel, cnt in: int16 [B][Hkv][n_sel][k_total] and [B][Hkv][n_sel] device.  Any order; entries that
+ *                hold no token of the context (negative, or at or past t_ctx) are skipped; a block
+ *                listed twice is attended once.
+ *   sm_scale   : logit scale, finite; normally 1/sqrt(D).
+ *   o      out : bf16 [B][Hq][n_nodes][D] device; zeros for an absent node or sequence.
+ *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_TREE_ATTN).
+ * o_i = softmax(sm_scale q_i K^T) V over the tokens t < t_ctx of node i's blocks and the tokens of
+ * A(i): bf16 inputs, float32 accumulation and online softmax.  Whatever the caches hold from t_ctx
+ * on, and whatever lies in the rows of absent nodes, has no effect.
+ */
+int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, const int32_t* t_ctx, int64_t t_max,
+                     const int32_t* parent, const void* k, const void* v, const void* k_tree, const void* v_tree,
+                     int32_t n_sel, const int16_t* sel, const int16_t* cnt, float sm_scale, void* o, void* ws,
+                     size_t ws_bytes, hipStream_t stream);
+
+/* Types of the probabilities of sparda_tree_verify. */
+enum sparda_prob_type { SPARDA_PROB_F32 = 0, SPARDA_PROB_BF16 = 1 };
+
+/*
+ * sparda_tree_verify -- which drafted tokens are kept, so that the kept tokens and the one that
+ * follows are distributed as if the target model had sampled them one by one.
+ *   vocab      : V >= 1, values per row of probabilities; ld >= V: elements from one row to the next.
+ *   p      in  : [B][n_nodes][ld] device of prob_type: row i is the target's distribution of the
+ *                token that follows node i.
+ *   q      in  : the same layout and type, or NULL.  Row i is the distribution from which the
+ *                children of node i were drawn, each independently of the others.  NULL: the
+ *                children were chosen, not drawn (the drafter's most likely ones, say).
+ *   tokens in  : int32 [B][n_nodes] device, the nodes' tokens (node 0's is not read).  A node whose
+ *                token is outside [0, V) is never accepted, nor are its descendants.
+ *   u      in  : float [B][n_nodes] device, uniform in [0, 1): u[i] tests node i, u[0] draws the
+ *                next token.
+ *   path   out : int32 [B][n_nodes] device: the accepted nodes from node 0 on, -1 padded.
+ *   n_path out : int32 [B] device: their number, >= 1; 0 for a sequence whose node 0 is absent.
+ *   next_token out: int32 [B] device; -1 where n_path is 0 or no weight is left.
+ *   ws, ws_bytes: device workspace of sparda_tree_verify_workspace_size() bytes.
+ * Per sequence: cur = 0, m = p_0, c = 1.  For the nodes i = 1, 2, .. whose parent is cur, with
+ * x = tokens[i]: node i is accepted if u_i c q_cur(x) < m(x) (q = 1 where q is NULL), and then
+ * cur = i, m = p_i, c = 1.  Otherwise the weights lose what was tested: m(y) = max(m(y) - c
+ * q_cur(y), 0) for all y and c = sum m; with q NULL, c = max(c - m(x), 0) and m(x) = 0.  next_token
+ * is the first y at which the running sum of m exceeds u_0 sum m.  If the last rejection left no
+ * weight at all it is undone for that draw; a rejection with q that leaves none is undone before
+ * the next sibling is tested.  A probability that is not a positive finite number counts as 0.
+ * Products, differences and sums are taken in float64.  Deterministic.
+ */
+int sparda_tree_verify(const sparda_shape* shape, int32_t n_nodes, int32_t vocab, int64_t ld, int32_t prob_type,
+                       const void* p, const void* q, const int32_t* tokens, const int32_t* parent, const float* u,
+                       int32_t* path, int32_t* n_path, int32_t* next_token, void* ws, size_t ws_bytes,
+                       hipStream_t stream);
+int sparda_tree_verify_workspace_size(const sparda_shape* shape, int32_t n_nodes, int32_t vocab, size_t* bytes);
+
+/*
+ * sparda_tree_commit -- packs the accepted path into the caches behind the context (the append of
+ * Alg. 2, for several tokens and layers at once), and computes the compressed keys of the windows
+ * that they complete (Sec. 3, Eq. 2; the incremental K~ update of Alg. 2).
+ *   path, n_path in: as sparda_tree_verify writes them.  Entries from the first one outside
+ *                [0, n_nodes) on, and tokens that would lie past t_cap, are dropped.
+ *   n_layers   : entries of the five tables, >= 1.  The tables are host arrays, read before the call
+ *                returns; what they point to is device memory:
+ *   k_tree, v_tree in: bf16 [B][Hkv][n_nodes][D], the nodes' K and V of each layer.
+ *   k_cache, v_cache in/out: bf16 [B][Hkv][t_cap][D]: token t_ctx + i becomes node path[i]'s;
+ *                nothing else is written.
+ *   k_cmp   out: bf16 [B][Hkv][nc_cap][D]: the windows that end in (t_ctx, t_new] and are < nc_cap,
+ *                the bits sparda_compress_keys gives.  The table may be NULL.
+ *   t_new   out: int32 [B] device, t_ctx plus the tokens written (t_ctx itself for an absent
+ *                sequence); not the array t_ctx.
+ * The buffers must not overlap.
+ */
+int sparda_tree_commit(const sparda_shape* shape, int32_t n_nodes, const int32_t* t_ctx, const int32_t* path,
+                       const int32_t* n_path, int32_t n_layers, const void* const* k_tree, const void* const* v_tree,
+                       void* const* k_cache, void* const* v_cache, void* const* k_cmp, int32_t* t_new,
+                       hipStream_t stream);
 
 /*
  * sparda_workspace_size -- device workspace bytes that call `op` (a sparda_op) needs for n_q

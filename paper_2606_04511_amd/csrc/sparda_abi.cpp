@@ -8,80 +8,15 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <mutex>
-#include <string>
 
+#include "abi_checks.hpp"
 #include "launch.hpp"
+#include "tree.hpp"
+
+using namespace sparda::abi;
 
 namespace {
-
-thread_local std::string g_detail;
-
-int fail(int status, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  std::vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_detail = buf;
-  return status;
-}
-
-int ok() {
-  g_detail.clear();
-  return SPARDA_OK;
-}
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-constexpr int64_t kMaxBlocks = 32768;  // block indices are int16
-
-int check_shape(const sparda_shape* s) {
-  if (!s) return fail(SPARDA_ERR_INVALID_ARG, "shape is null");
-  if (s->struct_size != sizeof(sparda_shape))
-    return fail(SPARDA_ERR_INVALID_ARG, "shape.struct_size is %u, expected %zu", s->struct_size, sizeof(sparda_shape));
-  if (s->batch < 1 || s->n_kv_heads < 1 || s->group_size < 1)
-    return fail(SPARDA_ERR_INVALID_ARG, "batch, n_kv_heads and group_size must be >= 1");
-  if (s->group_size > 16) return fail(SPARDA_ERR_UNSUPPORTED, "group_size %d > 16", s->group_size);
-  if (s->head_dim != 128) return fail(SPARDA_ERR_UNSUPPORTED, "head_dim %d (only 128)", s->head_dim);
-  if (s->block_size != 64) return fail(SPARDA_ERR_UNSUPPORTED, "block_size %d (only 64)", s->block_size);
-  if (!((s->cmp_kernel == 64 && s->cmp_stride == 64) || (s->cmp_kernel == 32 && s->cmp_stride == 16)))
-    return fail(SPARDA_ERR_UNSUPPORTED, "compression window (%d, %d) (only (64, 64) and (32, 16))", s->cmp_kernel,
-                s->cmp_stride);
-  if (s->n_init < 0 || s->n_local < 1) return fail(SPARDA_ERR_INVALID_ARG, "n_init >= 0 and n_local >= 1 required");
-  if ((int64_t)s->k_total < (int64_t)s->n_init + s->n_local)
-    return fail(SPARDA_ERR_INVALID_ARG, "k_total %d < n_init + n_local", s->k_total);
-  if (s->k_total >= kMaxBlocks) return fail(SPARDA_ERR_UNSUPPORTED, "k_total %d too large", s->k_total);
-  if (s->t_cap < 64 || s->t_cap % 64 != 0)
-    return fail(SPARDA_ERR_INVALID_ARG, "t_cap %lld must be a positive multiple of 64", (long long)s->t_cap);
-  if (s->t_cap / 64 > kMaxBlocks)
-    return fail(SPARDA_ERR_UNSUPPORTED, "t_cap %lld exceeds 32768 blocks", (long long)s->t_cap);
-  if (s->nc_cap < 0 || s->nc_cap > kMaxBlocks * (64 / s->cmp_stride))
-    return fail(SPARDA_ERR_INVALID_ARG, "nc_cap out of range");
-  if ((int64_t)s->batch * s->n_kv_heads > 65535)
-    return fail(SPARDA_ERR_UNSUPPORTED, "batch * n_kv_heads > 65535");
-  return SPARDA_OK;
-}
-
-int check_dev(const void* p, const char* name, uintptr_t align) {
-  if (!p) return fail(SPARDA_ERR_INVALID_ARG, "%s is null", name);
-  if (!aligned(p, align)) return fail(SPARDA_ERR_INVALID_ARG, "%s is not %zu-byte aligned", name, (size_t)align);
-  return SPARDA_OK;
-}
-
-int check_rows(const sparda_shape* s, int32_t n_q, int64_t q_pos0) {
-  if (n_q < 1) return fail(SPARDA_ERR_INVALID_ARG, "n_q %d < 1", n_q);
-  if (q_pos0 < 0 || q_pos0 + n_q > s->t_cap)
-    return fail(SPARDA_ERR_INVALID_ARG, "positions [%lld, %lld) outside t_cap %lld", (long long)q_pos0,
-                (long long)(q_pos0 + n_q), (long long)s->t_cap);
-  const int64_t rows = (int64_t)s->batch * s->n_kv_heads * n_q;
-  if (rows > (int64_t)1 << 30) return fail(SPARDA_ERR_UNSUPPORTED, "too many query rows");
-  return SPARDA_OK;
-}
-
-sparda::WinGrid grid_of(const sparda_shape* s) { return sparda::WinGrid{s->cmp_kernel, s->cmp_stride}; }
 
 // Workspace of sparda_forecast_select: window scores of the row-wise path (none for the fused
 // kernels).  The last row scores the most windows.
@@ -143,11 +78,6 @@ size_t attn_ws(const sparda_shape* s, int32_t n_q, int64_t q_pos0, int32_t* n_sp
   sparda::attn_plan(rows, s->k_total, n_splits, bps);
   if (*n_splits <= 1) return 0;
   return (size_t)rows * (size_t)*n_splits * (size_t)s->group_size * (size_t)(s->head_dim + 2) * sizeof(float);
-}
-
-int hip_status(hipError_t e, const char* what) {
-  if (e != hipSuccess) return fail(SPARDA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-  return ok();
 }
 
 // Scratch of sparda_sparse_attn_noalloc: the split partials of attention calls with fewer rows
@@ -323,6 +253,14 @@ int sparda_workspace_size(const sparda_shape* shape, int32_t op, int32_t n_q, in
   } else if (op == SPARDA_OP_DECODE_STEP) {
     if (n_q != 1) return fail(SPARDA_ERR_INVALID_ARG, "a decode step has n_q == 1");
     *bytes = step_ws(shape, q_pos0, nullptr);
+  } else if (op == SPARDA_OP_TREE_SELECT || op == SPARDA_OP_TREE_ATTN) {
+    if (n_q > sparda::kTreeMaxNodes)
+      return fail(SPARDA_ERR_UNSUPPORTED, "n_nodes %d > %d", n_q, sparda::kTreeMaxNodes);
+    const int64_t groups = (int64_t)shape->batch * shape->n_kv_heads;
+    if (op == SPARDA_OP_TREE_SELECT)
+      *bytes = sparda::tree_select_ws(groups, q_pos0, n_q, shape->n_init, shape->n_local);
+    else
+      *bytes = sparda::tree_attn_plan(groups, n_q, shape->group_size, shape->k_total, q_pos0).ws_bytes;
   } else {
     return fail(SPARDA_ERR_INVALID_ARG, "unknown op %d", op);
   }

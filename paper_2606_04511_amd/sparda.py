@@ -27,11 +27,16 @@ SPARDA_OP_SPARSE_ATTN = 2
 SPARDA_OP_MULTIHEAD_SELECT = 3
 SPARDA_OP_INDEXER_KL = 4
 SPARDA_OP_DECODE_STEP = 5
+SPARDA_OP_TREE_SELECT = 6
+SPARDA_OP_TREE_ATTN = 7
+SPARDA_PROB_F32 = 0
+SPARDA_PROB_BF16 = 1
 SPARDA_NOALLOC_SCRATCH_BYTES = 4718592  # the static scratch of sparda_sparse_attn_noalloc (include/sparda.h)
 
 EXPORTED = ("sparda_compress_keys", "sparda_forecast_select", "sparda_forecast_score_max", "sparda_multihead_select",
             "sparda_sparse_attn", "sparda_sparse_attn_noalloc", "sparda_gather_blocks", "sparda_stage_append_kv", "sparda_writeback_kv", "sparda_plan_staging", "sparda_indexer_kl",
-            "sparda_workspace_size", "sparda_status_string", "sparda_last_error_detail")
+            "sparda_tree_select", "sparda_tree_attn", "sparda_tree_verify", "sparda_tree_verify_workspace_size",
+            "sparda_tree_commit", "sparda_workspace_size", "sparda_status_string", "sparda_last_error_detail")
 
 
 class _CShape(ctypes.Structure):
@@ -105,7 +110,15 @@ def load() -> ctypes.CDLL:
         lib.sparda_writeback_kv.argtypes = [S, P, P, i32, i64, P, P, i32, P]
         lib.sparda_stage_append_kv.argtypes = [S, P, P, i64, P, P, P, P, P]
         lib.sparda_workspace_size.argtypes = [S, i32, i32, i64, ctypes.POINTER(ctypes.c_size_t)]
-        for name in ("sparda_compress_keys", "sparda_forecast_select", "sparda_forecast_score_max",
+        sz = ctypes.c_size_t
+        lib.sparda_tree_select.argtypes = [S, P, i32, P, i64, P, P, P, P, P, sz, P]
+        lib.sparda_tree_attn.argtypes = [S, P, i32, P, i64, P, P, P, P, P, i32, P, P, ctypes.c_float, P, P, sz, P]
+        lib.sparda_tree_verify.argtypes = [S, i32, i32, i64, i32, P, P, P, P, P, P, P, P, P, sz, P]
+        lib.sparda_tree_verify_workspace_size.argtypes = [S, i32, i32, ctypes.POINTER(sz)]
+        lib.sparda_tree_commit.argtypes = [S, i32, P, P, P, i32, P, P, P, P, P, P, P]
+        for name in ("sparda_tree_select", "sparda_tree_attn", "sparda_tree_verify",
+                     "sparda_tree_verify_workspace_size", "sparda_tree_commit",
+                     "sparda_compress_keys", "sparda_forecast_select", "sparda_forecast_score_max",
                      "sparda_multihead_select", "sparda_sparse_attn", "sparda_sparse_attn_noalloc", "sparda_decode_step",
                      "sparda_gather_blocks",
                      "sparda_stage_append_kv", "sparda_writeback_kv", "sparda_plan_staging", "sparda_indexer_kl",
@@ -247,3 +260,64 @@ def sparda_indexer_kl(shape: SpardaShape, q, k, f, k_cmp, n_q: int, q_pos0: int,
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_indexer_kl(ctypes.byref(cs), _p(q), _p(k), _p(f), _p(k_cmp), n_q, q_pos0, float(sm_scale),
                                     k_top, _p(loss), _p(d_f), _p(ws), ws_bytes, _stream(stream)), "sparda_indexer_kl")
+
+
+def sparda_tree_select(shape: SpardaShape, f, n_nodes: int, t_ctx, t_max: int, parent, k_cmp, sel, cnt, ws=None,
+                       ws_bytes: int = 0, stream=None):
+    cs = shape.c()
+    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
+        ws_bytes = ws.numel() * ws.element_size()
+    _check(load().sparda_tree_select(ctypes.byref(cs), _p(f), n_nodes, _p(t_ctx), t_max, _p(parent), _p(k_cmp), _p(sel),
+                                     _p(cnt), _p(ws), ws_bytes, _stream(stream)), "sparda_tree_select")
+
+
+def sparda_tree_attn(shape: SpardaShape, q, n_nodes: int, t_ctx, t_max: int, parent, k, v, k_tree, v_tree, n_sel: int,
+                     sel, cnt, sm_scale: float, o, ws=None, ws_bytes: int = 0, stream=None):
+    cs = shape.c()
+    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
+        ws_bytes = ws.numel() * ws.element_size()
+    _check(load().sparda_tree_attn(ctypes.byref(cs), _p(q), n_nodes, _p(t_ctx), t_max, _p(parent), _p(k), _p(v),
+                                   _p(k_tree), _p(v_tree), n_sel, _p(sel), _p(cnt), float(sm_scale), _p(o), _p(ws),
+                                   ws_bytes, _stream(stream)), "sparda_tree_attn")
+
+
+def sparda_tree_verify_workspace_size(shape: SpardaShape, n_nodes: int, vocab: int) -> int:
+    n = ctypes.c_size_t(0)
+    cs = shape.c()
+    _check(load().sparda_tree_verify_workspace_size(ctypes.byref(cs), n_nodes, vocab, ctypes.byref(n)),
+           "sparda_tree_verify_workspace_size")
+    return int(n.value)
+
+
+def sparda_tree_verify(shape: SpardaShape, n_nodes: int, vocab: int, ld: int, prob_type: int, p, q, tokens, parent, u,
+                       path, n_path, next_token, ws=None, ws_bytes: int = 0, stream=None):
+    cs = shape.c()
+    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
+        ws_bytes = ws.numel() * ws.element_size()
+    _check(load().sparda_tree_verify(ctypes.byref(cs), n_nodes, vocab, ld, prob_type, _p(p), _p(q), _p(tokens),
+                                     _p(parent), _p(u), _p(path), _p(n_path), _p(next_token), _p(ws), ws_bytes,
+                                     _stream(stream)), "sparda_tree_verify")
+
+
+def layer_pointers(tensors):
+    """The table of one pointer per layer that sparda_tree_commit takes.  It holds addresses: the tensors must stay
+    alive, and a table can be kept as long as they do."""
+    return (ctypes.c_void_p * len(tensors))(*[_p(x) for x in tensors])
+
+
+def _table(x, n_layers: int):
+    """A layer table: one made by layer_pointers, or a sequence of tensors."""
+    if x is None:
+        return None
+    if len(x) != n_layers:
+        raise ValueError(f"{len(x)} layers in a table of {n_layers}")
+    return x if isinstance(x, ctypes.Array) else layer_pointers(x)
+
+
+def sparda_tree_commit(shape: SpardaShape, n_nodes: int, t_ctx, path, n_path, n_layers: int, k_tree, v_tree, k_cache,
+                       v_cache, k_cmp, t_new, stream=None):
+    cs = shape.c()
+    _check(load().sparda_tree_commit(ctypes.byref(cs), n_nodes, _p(t_ctx), _p(path), _p(n_path), n_layers,
+                                     _table(k_tree, n_layers), _table(v_tree, n_layers), _table(k_cache, n_layers),
+                                     _table(v_cache, n_layers), _table(k_cmp, n_layers), _p(t_new), _stream(stream)),
+           "sparda_tree_commit")
