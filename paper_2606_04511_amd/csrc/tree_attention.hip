@@ -246,19 +246,21 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
         part[nt] = __ballot(vis[nt] != ~0u) != 0ull;
       }
       __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");  // this half's K (its V may be under way)
+      bf16x8 kf[2][4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+          kf[tt][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(kbuf + 4096 * tt + (ka ^ (ks << 6))));
       f32x4 st[NT][2];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        bf16x8 kf[4];
+      for (int nt = 0; nt < NT; ++nt) {
+        st[nt][0] = st[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (!on[nt]) continue;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) kf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(kbuf + 4096 * tt + (ka ^ (ks << 6))));
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          st[nt][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (!on[nt]) continue;
-#pragma unroll
-          for (int ks = 0; ks < 4; ++ks) st[nt][tt] = mfma16x16x32(kf[ks], qb[nt][ks], st[nt][tt]);
-        }
+          for (int tt = 0; tt < 2; ++tt) st[nt][tt] = mfma16x16x32(kf[tt][ks], qb[nt][ks], st[nt][tt]);
       }
       __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
       if (more) issue_k(j2, x2 & 1);
@@ -325,13 +327,17 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
             *reinterpret_cast<uint4*>(&lds.kv[wave][1][r * 256 + 16 * (lane & 15)]) = make_uint4(0u, 0u, 0u, 0u);
         wave_lds_sync();
       }
+      bf16x8 vf[8];
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) {
         const uint2 v0 = lds_read_tr16(vbuf + (va ^ (dt << 5))), v1 = lds_read_tr16(vbuf + 4096 + (va ^ (dt << 5)));
-        const bf16x8 vf = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
+        vf[dt] = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
+      }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          if (on[nt]) o[nt][dt] = mfma16x16x32(vf, pb[nt], o[nt][dt]);
+      for (int nt = 0; nt < NT; ++nt) {
+        if (!on[nt]) continue;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[nt][dt] = mfma16x16x32(vf[dt], pb[nt], o[nt][dt]);
       }
       __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
       if (more) issue_v(j2, x2 & 1);
