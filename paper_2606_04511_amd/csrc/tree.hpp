@@ -105,15 +105,15 @@ inline int tree_attn_tiles(int32_t n, int32_t group_size) {
   const int cols = n * group_size;
   return cols <= 16 ? 1 : 2;
 }
-// With fewer workgroups than CUs (one fits a CU) the blocks are split over them, at least one block per
-// wavefront each.
+// With fewer workgroups than CUs (one fits a CU) the blocks are split over them, at least half a block
+// per wavefront each.
 inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max) {
   const int cols = n * group_size, width = 16 * tree_attn_tiles(n, group_size);
   const int64_t wgs = groups * ((cols + width - 1) / width);
   const int64_t blocks = (t_max + 63) / 64 < k_total ? (t_max + 63) / 64 : k_total;
   int64_t ns = 1;
   if (wgs < 256) {
-    const int64_t want = (256 + wgs - 1) / wgs, most = (blocks + 1 + 7) / 8;
+    const int64_t want = (256 + wgs - 1) / wgs, most = (2 * blocks + 2 + 7) / 8;
     ns = want < most ? want : most;
     if (ns > 64) ns = 64;
   }

@@ -62,6 +62,22 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
   const int64_t bm = unit % n_groups;
   const int split = unit / n_groups;
   const int b = (int)(bm / a.n_kv_heads);
+  const int hh = lane & 15, grp = lane >> 4;
+  const int n_cols = n * G, c0 = tile * 16 * NT;
+  const int first_node = c0 / G, last_node = (min(c0 + 16 * NT, n_cols) - 1) / G;
+  // The tile's list entries: the first two of each thread are requested before anything is waited for.
+  const int rows = a.n_sel == 1 ? 1 : last_node - first_node + 1;
+  const int64_t row0 = a.n_sel == 1 ? bm : bm * n + first_node;
+  const int n_listed = rows * a.k_total;
+  auto list_row = [&](int e) { return e / a.k_total; };
+  auto list_entry = [&](int e) {  // the block, or -1; the count and the entry are requested together
+    const int r = list_row(e), j = a.sel[row0 * a.k_total + e], c = a.cnt[row0 + r];
+    return e - r * a.k_total < c ? j : -1;
+  };
+  constexpr int kAhead = 2;
+  int ahead[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) ahead[i] = list_entry(min(tid + kTaThreads * i, n_listed - 1));
   const int64_t ctx = tree_context(a.tb, b);
   uint64_t anc = tree_ancestors(a.tb.parent + (int64_t)b * n, n, lane);
   if (ctx < 0) anc = 0ull;
@@ -69,9 +85,6 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
   const uint64_t present = __ballot(anc != 0ull);
 
   // ---- the lane's columns (those past the last repeat it) and their queries
-  const int hh = lane & 15, grp = lane >> 4;
-  const int n_cols = n * G, c0 = tile * 16 * NT;
-  const int first_node = c0 / G, last_node = (min(c0 + 16 * NT, n_cols) - 1) / G;
   uint64_t col_anc[NT];
   int col_node[NT];  // from the tile's first node
   bf16x8 qb[NT][4];
@@ -154,18 +167,18 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
     __syncthreads();  // the last window's are no longer read
     for (int i = tid; i < wn; i += kTaThreads) lds.table[i] = 0ull;
     __syncthreads();
-    const int rows = a.n_sel == 1 ? 1 : last_node - first_node + 1;
-    const int64_t row0 = a.n_sel == 1 ? bm : bm * n + first_node;
-    for (int e = tid; e < rows * a.k_total; e += kTaThreads) {
-      const int r = e / a.k_total, s = e - r * a.k_total;
-      const int j = s < (int)a.cnt[row0 + r] ? (int)a.sel[(row0 + r) * a.k_total + s] - w0 : -1;
-      if (j >= 0 && j < wn) {
-        if (a.n_sel == 1)
-          lds.table[j] = ~0ull;
-        else if ((present >> (first_node + r)) & 1ull)
-          atomicOr(reinterpret_cast<unsigned long long*>(&lds.table[j]), 1ull << r);
-      }
-    }
+    auto mark = [&](int e, int block) {
+      const int j = block - w0, r = list_row(e);
+      if (block < 0 || j < 0 || j >= wn) return;
+      if (a.n_sel == 1)
+        lds.table[j] = ~0ull;
+      else if ((present >> (first_node + r)) & 1ull)
+        atomicOr(reinterpret_cast<unsigned long long*>(&lds.table[j]), 1ull << r);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (tid + kTaThreads * i < n_listed) mark(tid + kTaThreads * i, ahead[i]);
+    for (int e = tid + kTaThreads * kAhead; e < n_listed; e += kTaThreads) mark(e, list_entry(e));
     __syncthreads();
     constexpr int kRounds = kTaWindow / kTaThreads;
     uint64_t listed[kRounds];

@@ -25,37 +25,115 @@ __device__ __forceinline__ SeqGeom seq_geom(const TreeBatch& tb, int b, int lane
   return {t, t < 0 ? 0 : (int)__popcll(anc)};
 }
 
-// Block scores of one node, 16 candidates per workgroup: 16 lanes per candidate, 8 dims each.
-__global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a) {
-  const int64_t row = blockIdx.x;
-  const int i = (int)(row % a.tb.n);
-  const int64_t bm = row / a.tb.n;
-  const int b = (int)(bm / a.n_kv_heads);
-  const int lane = threadIdx.x & 63;
-  const SeqGeom s = seq_geom(a.tb, b, lane);
-  const int depth = readlane_i(s.depth, i);
-  if (depth == 0) return;
-  const RowGeom g = row_geom(s.t + depth - 1, a.n_init, a.n_local, a.k_total);
+// Block scores of all nodes of a (batch, group) on MFMA: the keys are read once.  A = 16 nodes' Forecast
+// rows (MT of them in registers), B = 16 keys, so consecutive candidates lie in consecutive lanes.  A step
+// is 64 keys, all requested before the first product: 64 blocks on the one-key-per-block grid, 16 blocks
+// of the (32, 16) grid as four tiles, tile u holding window u of each block.  Window -1 of a block is
+// window 3 of the one before: the neighbouring lane's score, or for lane 0 that of the last step (at a
+// wavefront's first step one more key).
+template <bool kBlocks, int MT>
+__global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n_groups, int steps) {
+  constexpr int kPerStep = kBlocks ? 64 : 16;  // candidates
+  const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t bm = blockIdx.x % n_groups;
+  const int part = (int)(blockIdx.x / n_groups) * 4 + wave;
+  const int n = a.tb.n;
+  const int64_t t = tree_context(a.tb, (int)(bm / a.n_kv_heads));
+  if (t < 0) return;
+  // the candidates of the deepest node there can be: no other node has more
+  const RowGeom g = row_geom(t + n - 1, a.n_init, a.n_local, a.k_total);
   if (g.n_take >= g.n_cand) return;
-  const int32_t vis = grid_win_vis(a.grid, s.t - 1);
-  const int c = threadIdx.x & 15;
-  const int x = blockIdx.y * 16 + (threadIdx.x >> 4);
-  if (x >= g.n_cand) return;
-  const uint4 fw = ld16(a.f + row * kHeadDim + c * 8);
-  const float fv[8] = {bf16lo(fw.x), bf16hi(fw.x), bf16lo(fw.y), bf16hi(fw.y),
-                       bf16lo(fw.z), bf16hi(fw.z), bf16lo(fw.w), bf16hi(fw.w)};
-  const int lo = grid_win_lo(a.grid, g.cand_lo + x), hi = min(grid_win_hi(a.grid, g.cand_lo + x), vis);
-  float best = -INFINITY;
-  for (int w = lo; w <= hi; ++w) {
-    const uint4 kw = ld16(a.kc + (bm * a.nc_cap + w) * kHeadDim + c * 8);
-    const float kv[8] = {bf16lo(kw.x), bf16hi(kw.x), bf16lo(kw.y), bf16hi(kw.y),
-                         bf16lo(kw.z), bf16hi(kw.z), bf16lo(kw.w), bf16hi(kw.w)};
-    float d = 0.f;
+  const int x_end = min(g.n_cand, (part + 1) * steps * kPerStep);
+  int x0 = part * steps * kPerStep;
+  if (x0 >= x_end) return;
+  const int32_t vis = grid_win_vis(a.grid, t - 1);  // nothing past it is read
+  bf16x8 fa[MT][4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d = fmaf(fv[e], kv[e], d);
-    best = fmaxf(best, row16_sum(d));
+  for (int mt = 0; mt < MT; ++mt) {
+    const uint16_t* src = a.f + (bm * n + min(16 * mt + c, n - 1)) * kHeadDim + 8 * q;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) fa[mt][ks] = as_bf16x8(ld16(src + 32 * ks));
   }
-  if (c == 0) a.ws[row * a.ws_stride + x] = best;
+  const uint16_t* keys = a.kc + bm * a.nc_cap * kHeadDim + 8 * q;
+  auto key_at = [&](int w) { return keys + (int64_t)max(min(w, vis), 0) * kHeadDim; };
+  auto products = [&](const uint4* kw, int mt) {
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) s = mfma16x16x32(fa[mt][ks], as_bf16x8(kw[ks]), s);
+    return s;
+  };
+  float* const out = a.ws + bm * n * a.ws_stride;
+  auto store = [&](int mt, int x, const f32x4& s) {  // element i: node 16 mt + 4 q + i, candidate x + c
+    if (x + c >= g.n_cand) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int node = 16 * mt + 4 * q + i;
+      if (node < n) out[node * a.ws_stride + x + c] = s[i];
+    }
+  };
+  f32x4 carry[MT];
+  if constexpr (!kBlocks) {
+    const int w = 4 * (g.cand_lo + x0) - 1;
+    uint4 kw[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) kw[ks] = ld16(key_at(w) + 32 * ks);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      carry[mt] = products(kw, mt);
+      if (w < 0 || w > vis) carry[mt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    }
+  }
+  for (; x0 < x_end; x0 += kPerStep) {
+    uint4 kw[4][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint16_t* src = key_at(kBlocks ? g.cand_lo + x0 + 16 * u + c : 4 * (g.cand_lo + x0 + c) + u);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) kw[u][ks] = ld16_nt(src + 32 * ks);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if constexpr (kBlocks) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) store(mt, x0 + 16 * u, products(kw[u], mt));
+      } else {
+        f32x4 best, s;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          s = products(kw[u], mt);
+          if (4 * (g.cand_lo + x0 + c) + u > vis) s = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) best[i] = u == 0 ? s[i] : fmaxf(best[i], s[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int before = __builtin_amdgcn_update_dpp(__float_as_int(carry[mt][i]), __float_as_int(s[i]), 0x111, 0xf, 0xf, false);
+          best[i] = fmaxf(best[i], __int_as_float(before));  // row_shr:1, lane 0 keeps the carry
+          carry[mt][i] = dpp_f<0x121>(s[i]);                 // row_ror:1: lane 15's to lane 0
+        }
+        store(mt, x0, best);
+      }
+    }
+  }
+}
+
+template <bool kBlocks>
+hipError_t launch_scores(const TreeSelectArgs& a, int C, hipStream_t stream) {
+  const int groups = a.tb.batch * a.n_kv_heads;
+  const int total = (C + (kBlocks ? 64 : 16) - 1) / (kBlocks ? 64 : 16);
+  // steps per wavefront: one while the chip is not full, at most 8
+  const int64_t all = (int64_t)groups * total;
+  const int steps = (int)(all <= 8192 ? 1 : all >= 65536 ? 8 : all / 8192);
+  const int parts = (total + steps - 1) / steps;
+  const dim3 grid((unsigned)(groups * ((parts + 3) / 4))), block(256);
+  switch ((a.tb.n + 15) / 16) {
+    case 1: hipLaunchKernelGGL((tree_score_kernel<kBlocks, 1>), grid, block, 0, stream, a, groups, steps); break;
+    case 2: hipLaunchKernelGGL((tree_score_kernel<kBlocks, 2>), grid, block, 0, stream, a, groups, steps); break;
+    case 3: hipLaunchKernelGGL((tree_score_kernel<kBlocks, 3>), grid, block, 0, stream, a, groups, steps); break;
+    default: hipLaunchKernelGGL((tree_score_kernel<kBlocks, 4>), grid, block, 0, stream, a, groups, steps);
+  }
+  return hipGetLastError();
 }
 
 // One wavefront per node: forced blocks, padding, count, and the exact top-k over its block scores, in
@@ -116,8 +194,7 @@ hipError_t launch_tree_select(const TreeSelectArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.tb.batch * a.n_kv_heads * a.tb.n;
   const int C = row_geom(a.tb.t_max + a.tb.n - 1, a.n_init, a.n_local, a.k_total).n_cand;
   if (C > 0) {
-    hipLaunchKernelGGL(tree_score_kernel, dim3((unsigned)rows, (unsigned)((C + 15) / 16)), dim3(256), 0, stream, a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = grid_is_blocks(a.grid) ? launch_scores<true>(a, C, stream) : launch_scores<false>(a, C, stream);
     if (e != hipSuccess) return e;
   }
   const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
