@@ -123,10 +123,12 @@ inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size
 
 // Workspace of the verification: per sequence the state that the walk left and the sums of the
 // row's pieces.
-constexpr int kVerifyPiece = 4096;
+constexpr int kVerifyPiece = 1024;
+inline int32_t tree_verify_pieces(int32_t vocab) {  // a row may begin up to 3 elements past a piece's first
+  return (int32_t)(((int64_t)vocab + 3 + kVerifyPiece - 1) / kVerifyPiece);
+}
 inline size_t tree_verify_ws(int64_t batch, int32_t vocab) {
-  const size_t pieces = ((size_t)vocab + 7 + kVerifyPiece - 1) / kVerifyPiece;
-  return (size_t)batch * (64 * sizeof(double) + 2 * pieces * sizeof(double) + 64);
+  return (size_t)batch * (64 * sizeof(double) + 2 * (size_t)tree_verify_pieces(vocab) * sizeof(double) + 64);
 }
 
 hipError_t launch_tree_select(const TreeSelectArgs& a, hipStream_t stream);

@@ -1,12 +1,13 @@
 // tree_verify.hip -- verification of drafted tokens against the target's probabilities from given
 // random numbers (include/sparda.h states the rule).
 //
-// Two launches.  Every workgroup of the first walks the tree of its sequence by itself: lane i of each
-// wavefront holds node i's parent, token, random number and two probabilities, all requested at once,
-// and the walk itself is scalar.  Only a second sibling's test after a rejection with q needs the sum of
-// a whole row of remaining weights, which the workgroup then takes.  The workgroups of a sequence come
-// to the same result, and each sums the final row's weights over its pieces of 4096 tokens.  The
-// second launch finds the piece in which the running sum passes u_0 times the total, and the token.
+// Every workgroup walks the tree of its sequence by itself: lane i of each wavefront holds node i's
+// parent, token, random number and two probabilities, all requested at once, and the walk is scalar.  Only
+// a second sibling's test after a rejection with q needs the sum of a whole row of remaining weights, which
+// the workgroup then takes.  The workgroups of a sequence come to the same result, and their wavefronts
+// share the final row: each sums the weights of pieces of 1024 tokens.  One wavefront then finds the
+// piece in which the running sum passes u_0 times the total, and the token: in the same launch where one
+// workgroup has all pieces, else in a second one.
 //
 // float64 throughout: a running sum over a vocabulary in float32 is off by more than most tokens weigh.
 #include "device_util.hpp"
@@ -17,10 +18,13 @@ namespace sparda {
 
 namespace {
 
-constexpr int kWalkThreads = 512;
-constexpr int kPickThreads = 1024;
+// Wavefronts of a workgroup: with q more of them, for the sums of whole rows inside the walk.
+template <bool kQ>
+constexpr int kWalkWaves = kQ ? 16 : 8;
+constexpr int kPickPieces = 16;              // most pieces that one workgroup takes from walk to token
+constexpr int kPerLane = kVerifyPiece / 64;  // consecutive tokens of a piece that a lane holds
 
-// What the walk leaves in the workspace for the second launch.
+// What the walk leaves for the pick.
 struct VerifyState {
   int32_t cur, rounds;   // the last accepted node (-1: none); rejections with q that stand there
   int32_t last;          // the node rejected last, or -1
@@ -43,7 +47,10 @@ __host__ __device__ inline VerifyWs verify_ws(void* ws, int64_t batch) {
 }
 static_assert(sizeof(VerifyState) <= 64, "tree_verify_ws");
 
-__device__ __forceinline__ double weight_of(float x) { return x > 0.f && x < INFINITY ? (double)x : 0.0; }
+// A probability that is not a positive finite number counts as 0.  (Bits 1 .. 0x7f7fffff are the positive finite ones.)
+__device__ __forceinline__ double weight_of(float x) {
+  return (double)(__float_as_uint(x) - 1u < 0x7f7fffffu ? x : 0.f);
+}
 
 template <bool kBf16>
 __device__ __forceinline__ double prob_at(const void* base, int64_t at) {
@@ -57,26 +64,43 @@ __device__ __forceinline__ int row_shift(const void* base, int64_t at) {
   return (int)((reinterpret_cast<uintptr_t>(base) / (kBf16 ? 2 : 4) + (uintptr_t)at) & 3);
 }
 
-// The row's elements e .. e + 3, of which those outside [0, vocab) are 0; e + its shift is a multiple of 4.
+// The kPerLane elements of a row from e on, of which those outside [0, vocab) are 0; e plus the row's shift is a
+// multiple of 4.  One branch, so that all the loads of a lane inside the row are in flight together.
 template <bool kBf16>
-__device__ __forceinline__ void load4(const void* base, int64_t row, int64_t e, int vocab, double* x) {
-  if (e >= 0 && e + 4 <= vocab) {
+__device__ __forceinline__ void load_piece(const void* base, int64_t row, int64_t e, int vocab, double* x) {
+  if (e >= 0 && e + kPerLane <= vocab) {
     if constexpr (kBf16) {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row + e);
-      x[0] = weight_of(bf16lo(w.x));
-      x[1] = weight_of(bf16hi(w.x));
-      x[2] = weight_of(bf16lo(w.y));
-      x[3] = weight_of(bf16hi(w.y));
+      uint2 w[kPerLane / 4];
+#pragma unroll
+      for (int k = 0; k < kPerLane / 4; ++k)
+        w[k] = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row + e + 4 * k);
+#pragma unroll
+      for (int k = 0; k < kPerLane / 4; ++k) {
+        x[4 * k] = weight_of(bf16lo(w[k].x));
+        x[4 * k + 1] = weight_of(bf16hi(w[k].x));
+        x[4 * k + 2] = weight_of(bf16lo(w[k].y));
+        x[4 * k + 3] = weight_of(bf16hi(w[k].y));
+      }
     } else {
-      const float4 w = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + row + e);
-      x[0] = weight_of(w.x);
-      x[1] = weight_of(w.y);
-      x[2] = weight_of(w.z);
-      x[3] = weight_of(w.w);
+      float4 w[kPerLane / 4];
+#pragma unroll
+      for (int k = 0; k < kPerLane / 4; ++k)
+        w[k] = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + row + e + 4 * k);
+#pragma unroll
+      for (int k = 0; k < kPerLane / 4; ++k) {
+        x[4 * k] = weight_of(w[k].x);
+        x[4 * k + 1] = weight_of(w[k].y);
+        x[4 * k + 2] = weight_of(w[k].z);
+        x[4 * k + 3] = weight_of(w[k].w);
+      }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = e + i >= 0 && e + i < vocab ? prob_at<kBf16>(base, row + e + i) : 0.0;
+    for (int k = 0; k < kPerLane; ++k) {
+      const bool in = e + k >= 0 && e + k < vocab;
+      const double y = prob_at<kBf16>(base, row + (in ? e + k : 0));
+      x[k] = in ? y : 0.0;
+    }
   }
 }
 
@@ -85,7 +109,7 @@ __device__ __forceinline__ double left_of(double m, double q, const double* c, i
 #pragma clang fp contract(off)
   for (int r = 0; r < rounds; ++r) {
     const double cut = c[r] * q;
-    m = m - cut > 0.0 ? m - cut : 0.0;
+    m = fmax(m - cut, 0.0);
   }
   return m;
 }
@@ -115,13 +139,108 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
   return s;
 }
 
+__device__ __forceinline__ double readlane_sum(double x) { return readlane_d(wave_sum(x), 0); }
+
+// Inclusive running sum over the wavefront's lanes.
+__device__ __forceinline__ double wave_scan(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// A lane's kPerLane weights of a piece that begins at element e0 of the row (a multiple of 4 with the row's shift),
+// after `rounds` rejections with q.
 template <bool kBf16, bool kQ>
-__global__ __launch_bounds__(kWalkThreads) void tree_walk_kernel(TreeVerifyArgs a, int n_pieces) {
+__device__ __forceinline__ void piece_weights(const TreeVerifyArgs& a, int64_t row, int64_t e0, const double* c,
+                                              int rounds, double* x) {
+  const int lane = threadIdx.x & 63;
+  load_piece<kBf16>(a.p, row, e0 + kPerLane * lane, a.vocab, x);
+  if constexpr (kQ) {
+    if (rounds > 0) {
+      double y[kPerLane];
+      load_piece<kBf16>(a.q, row, e0 + kPerLane * lane, a.vocab, y);
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) x[k] = left_of(x[k], y[k], c, rounds);
+    }
+  }
+}
+
+// The next token, by one wavefront: the pieces' sums, the piece, the token.  sums: [n_pieces][2], global or LDS.
+template <bool kBf16, bool kQ>
+__device__ __forceinline__ int pick_token(const TreeVerifyArgs& a, int b, const VerifyState& st, const double* c,
+                                          const double* sums, int n_pieces) {
+  const int lane = threadIdx.x & 63;
+  double s1 = 0.0, s0 = 0.0;
+  for (int i = lane; i < n_pieces; i += 64) {
+    s1 += sums[2 * i];
+    s0 += sums[2 * i + 1];
+  }
+  s1 = readlane_sum(s1);
+  s0 = readlane_sum(s0);
+  const int undone = s1 > 0.0 ? 0 : 1;  // the last rejection left nothing: it does not count
+  const double total = undone ? s0 : s1;
+  if (!(total > 0.0)) return -1;
+  const double goal = (double)a.u[(int64_t)b * a.n] * total;
+  // the first piece whose running sum exceeds the goal, else the last that weighs anything
+  int piece = -1;
+  double before = 0.0, carry = 0.0;
+  for (int i0 = 0; i0 < n_pieces; i0 += 64) {
+    const double x = i0 + lane < n_pieces ? sums[2 * (i0 + lane) + undone] : 0.0;
+    const double run = carry + wave_scan(x);
+    const uint64_t heavy = __ballot(x > 0.0), over = __ballot(x > 0.0 && run > goal);
+    const int at = over ? (int)__builtin_ctzll(over) : heavy ? 63 - (int)__builtin_clzll(heavy) : -1;
+    if (at >= 0) {
+      piece = i0 + at;
+      before = at == 0 ? carry : readlane_d(run, at - 1);
+    }
+    if (over) break;
+    carry = readlane_d(run, 63);
+  }
+  const int64_t row = ((int64_t)b * a.n + st.cur) * a.ld;
+  const int64_t e = (int64_t)piece * kVerifyPiece - row_shift<kBf16>(a.p, row) + kPerLane * lane;
+  double x[kPerLane];
+  piece_weights<kBf16, kQ>(a, row, e - kPerLane * lane, c, st.rounds - (st.rounds > 0 ? undone : 0), x);
+  if constexpr (!kQ) {
+    uint64_t rejected = st.rejected;
+    if (undone && st.last >= 0) rejected &= ~(1ull << st.last);
+    for (; rejected; rejected &= rejected - 1) {
+      const int64_t y = a.tokens[(int64_t)b * a.n + (int)__builtin_ctzll(rejected)];
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) x[k] = e + k == y ? 0.0 : x[k];
+    }
+  }
+  double own = 0.0;
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) own += x[k];
+  const double run = before + wave_scan(own), up = __shfl_up(run, 1, 64);
+  double mine = lane == 0 ? before : up;
+  int first = -1, last = -1;  // the lane's first token past the goal, and its last that weighs anything
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) {
+    mine += x[k];
+    if (x[k] > 0.0) {
+      last = (int)(e + k);
+      if (first < 0 && mine > goal) first = last;
+    }
+  }
+  const uint64_t hit = __ballot(first >= 0), any = __ballot(last >= 0);
+  if (hit) return readlane_i(first, (int)__builtin_ctzll(hit));
+  return any ? readlane_i(last, 63 - (int)__builtin_clzll(any)) : -1;
+}
+
+// kPick: one workgroup per sequence, which finds the token too.
+template <bool kBf16, bool kQ, bool kPick>
+__global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVerifyArgs a, int n_pieces) {
 #pragma clang fp contract(off)
-  constexpr int NW = kWalkThreads / 64;
+  constexpr int NW = kWalkWaves<kQ>;
   __shared__ double cs[NW][64];   // each wavefront's copy
   __shared__ double part[NW];
-  __shared__ uint32_t gone[kVerifyPiece / 32];
+  __shared__ uint32_t gone[NW][kVerifyPiece / 32];
+  __shared__ double piece_sums[kPick ? 2 * kPickPieces : 2];
   __shared__ int slots[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int b = blockIdx.y, n = a.n;
@@ -150,12 +269,11 @@ __global__ __launch_bounds__(kWalkThreads) void tree_walk_kernel(TreeVerifyArgs 
         const int64_t row = (node0 + cur) * a.ld;
         const int shift = row_shift<kBf16>(a.p, row);
         double s = 0.0;
-        for (int64_t e = 4 * (int)threadIdx.x - shift; e < a.vocab; e += 4 * kWalkThreads) {
-          double x[4], y[4];
-          load4<kBf16>(a.p, row, e, a.vocab, x);
-          load4<kBf16>(a.q, row, e, a.vocab, y);
+        for (int piece = wave; piece < n_pieces; piece += NW) {
+          double x[kPerLane];
+          piece_weights<kBf16, true>(a, row, (int64_t)piece * kVerifyPiece - shift, cs[wave], rounds, x);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) s += left_of(x[k], y[k], cs[wave], rounds);
+          for (int k = 0; k < kPerLane; ++k) s += x[k];
         }
         s = block_sum<NW>(s, part);
         if (s > 0.0)
@@ -193,205 +311,106 @@ __global__ __launch_bounds__(kWalkThreads) void tree_walk_kernel(TreeVerifyArgs 
   }
   const bool present = readlane_i((int)(uint32_t)anc, 0) != 0;
   const VerifyWs ws = verify_ws(a.ws, a.batch);
+  const VerifyState state = {present ? cur : -1, rounds, last, 0, rejected};
   if (blockIdx.x == 0 && wave == 0) {
     slots[lane] = -1;
     wave_lds_sync();
     if (present && ((kept >> lane) & 1ull)) slots[mbcnt64(kept)] = lane;
     wave_lds_sync();
     if (lane < n) a.path[node0 + lane] = slots[lane];
-    if constexpr (kQ) ws.c[(int64_t)b * 64 + lane] = cs[0][lane];
+    if constexpr (kQ && !kPick) ws.c[(int64_t)b * 64 + lane] = cs[0][lane];
     if (lane == 0) {
       a.n_path[b] = present ? (int)__popcll(kept) : 0;
-      ws.state[b] = {present ? cur : -1, rounds, last, 0, rejected};
+      if constexpr (!kPick) ws.state[b] = state;
+      if (!present) a.next_token[b] = -1;
     }
   }
   if (!present) return;
-  // ---- the final row's weights, piece by piece
+  // ---- the final row's weights: a piece per wavefront at a time
   const int64_t row = (node0 + cur) * a.ld;
   const int shift = row_shift<kBf16>(a.p, row);
-  for (int piece = blockIdx.x; piece < n_pieces; piece += gridDim.x) {
+  double* const sums = kPick ? piece_sums : ws.sums + (int64_t)b * n_pieces * 2;
+  for (int piece = blockIdx.x * NW + wave; piece < n_pieces; piece += gridDim.x * NW) {
     const int64_t e0 = (int64_t)piece * kVerifyPiece - shift;
-    double s1 = 0.0, s0 = 0.0;
-    if constexpr (!kQ) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < kVerifyPiece / 32; i += kWalkThreads) gone[i] = 0u;
-      __syncthreads();
-      if (wave == 0 && ((rejected >> lane) & 1ull)) {
-        const int64_t x = tok - e0;
-        if (x >= 0 && x < kVerifyPiece) atomicOr(&gone[x >> 5], 1u << (x & 31));
-      }
-      __syncthreads();
-    }
-    for (int at = 4 * threadIdx.x; at < kVerifyPiece; at += 4 * kWalkThreads) {
-      double x[4];
-      load4<kBf16>(a.p, row, e0 + at, a.vocab, x);
-      if constexpr (kQ) {
-        double y[4];
-        if (rounds > 0) load4<kBf16>(a.q, row, e0 + at, a.vocab, y);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const double w0 = rounds > 0 ? left_of(x[k], y[k], cs[wave], rounds - 1) : x[k];
-          s0 += w0;
-          s1 += rounds > 0 ? left_of(w0, y[k], cs[wave] + rounds - 1, 1) : w0;
-        }
-      } else {
-        const uint32_t bits = gone[at >> 5] >> (at & 31);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s1 += (bits >> k) & 1u ? 0.0 : x[k];
-      }
-    }
-    s1 = block_sum<NW>(s1, part);
+    double x[kPerLane], s1 = 0.0, s0 = 0.0;
+    piece_weights<kBf16, kQ>(a, row, e0, cs[wave], rounds > 0 ? rounds - 1 : 0, x);
     if constexpr (kQ) {
-      s0 = block_sum<NW>(s0, part);
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) s0 += x[k];
+      s0 = wave_sum(s0);
+      s1 = s0;
+      if (rounds > 0) {
+        double y[kPerLane];
+        load_piece<kBf16>(a.q, row, e0 + kPerLane * lane, a.vocab, y);
+        s1 = 0.0;
+#pragma unroll
+        for (int k = 0; k < kPerLane; ++k) s1 += left_of(x[k], y[k], cs[wave] + rounds - 1, 1);
+        s1 = wave_sum(s1);
+      }
     } else {
-      s0 = s1;
+      if (rejected != 0ull) {  // rejected tokens of the piece weigh nothing
+        if (lane < kVerifyPiece / 32) gone[wave][lane] = 0u;
+        wave_lds_sync();
+        const int64_t at = tok - e0;
+        if (((rejected >> lane) & 1ull) && at >= 0 && at < kVerifyPiece) atomicOr(&gone[wave][at >> 5], 1u << (at & 31));
+        wave_lds_sync();
+        const uint32_t bits = gone[wave][lane * kPerLane / 32] >> (lane * kPerLane % 32);
+#pragma unroll
+        for (int k = 0; k < kPerLane; ++k) x[k] = (bits >> k) & 1u ? 0.0 : x[k];
+      }
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) s1 += x[k];
+      s1 = s0 = wave_sum(s1);
       if (last >= 0) {  // the last rejected token, unless an earlier rejection took its weight
-        const int x = readlane_i(tok, last);
-        const uint64_t same = __ballot(((rejected >> lane) & 1ull) && tok == x);
-        if (x - e0 >= 0 && x - e0 < kVerifyPiece && __popcll(same) == 1) s0 += readlane_d(pv, last);
+        const int y = readlane_i(tok, last);
+        const uint64_t same = __ballot(((rejected >> lane) & 1ull) && tok == y);
+        if (y - e0 >= 0 && y - e0 < kVerifyPiece && __popcll(same) == 1) s0 += readlane_d(pv, last);
       }
     }
-    if (threadIdx.x == 0) {
-      double* out = ws.sums + ((int64_t)b * n_pieces + piece) * 2;
-      out[0] = s1;
-      out[1] = s0;
+    if (lane == 0) {
+      sums[2 * piece] = s1;
+      sums[2 * piece + 1] = s0;
     }
   }
-}
-
-// Inclusive running sum over the workgroup's threads.
-template <int NW>
-__device__ __forceinline__ double block_scan(double x, double* part, double* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
+  if constexpr (kPick) {
+    __syncthreads();
+    if (wave == 0) {
+      const int token = pick_token<kBf16, kQ>(a, b, state, cs[0], piece_sums, n_pieces);
+      if (lane == 0) a.next_token[b] = token;
+    }
   }
-  __syncthreads();
-  if (lane == 63) part[wave] = x;
-  __syncthreads();
-  double before = 0.0, all = 0.0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    before += w < wave ? part[w] : 0.0;
-    all += part[w];
-  }
-  *total = all;
-  return before + x;
 }
 
 template <bool kBf16, bool kQ>
-__global__ __launch_bounds__(kPickThreads) void tree_pick_kernel(TreeVerifyArgs a, int n_pieces) {
+__global__ __launch_bounds__(64) void tree_pick_kernel(TreeVerifyArgs a, int n_pieces) {
 #pragma clang fp contract(off)
-  constexpr int NW = kPickThreads / 64;
-  __shared__ double part[NW];
   __shared__ double cs[64];
-  __shared__ double at_piece;
-  __shared__ int found, spare;
-  const int b = blockIdx.x, tid = threadIdx.x;
+  const int b = blockIdx.x, lane = threadIdx.x;
   const VerifyWs ws = verify_ws(a.ws, a.batch);
   const VerifyState st = ws.state[b];
-  if (st.cur < 0) {
-    if (tid == 0) a.next_token[b] = -1;
-    return;
-  }
-  const double* sums = ws.sums + (int64_t)b * n_pieces * 2;
-  if (kQ && tid < 64) cs[tid] = ws.c[(int64_t)b * 64 + tid];
-  double s1 = 0.0, s0 = 0.0;
-  for (int i = tid; i < n_pieces; i += kPickThreads) {
-    s1 += sums[2 * i];
-    s0 += sums[2 * i + 1];
-  }
-  s1 = block_sum<NW>(s1, part);
-  s0 = block_sum<NW>(s0, part);
-  const int undone = s1 > 0.0 ? 0 : 1;  // the last rejection left nothing: it does not count
-  const double total = undone ? s0 : s1;
-  if (!(total > 0.0)) {
-    if (tid == 0) a.next_token[b] = -1;
-    return;
-  }
-  const double goal = (double)a.u[(int64_t)b * a.n] * total;
-  // ---- the piece: the first whose running sum exceeds the goal, else the last that weighs anything
-  if (tid == 0) {
-    found = 0x7fffffff;
-    spare = -1;
-  }
-  double carry = 0.0;
-  for (int i0 = 0; i0 < n_pieces; i0 += kPickThreads) {
-    const int i = i0 + tid;
-    const double x = i < n_pieces ? sums[2 * i + undone] : 0.0;
-    double all;
-    const double run = carry + block_scan<NW>(x, part, &all);
-    if (x > 0.0) {
-      if (run > goal) atomicMin(&found, i);
-      atomicMax(&spare, i);
-    }
-    carry += all;
-    __syncthreads();
-    if (found != 0x7fffffff) break;
-  }
-  const int piece = found != 0x7fffffff ? found : spare;
-  carry = 0.0;
-  for (int i0 = 0; i0 < n_pieces; i0 += kPickThreads) {  // what lies before it
-    const int i = i0 + tid;
-    double all;
-    const double x = i < n_pieces ? sums[2 * i + undone] : 0.0;
-    const double run = carry + block_scan<NW>(x, part, &all);
-    if (i == piece) at_piece = run - x;
-    carry += all;
-  }
+  if constexpr (kQ) cs[lane] = ws.c[(int64_t)b * 64 + lane];
+  if (st.cur < 0) return;
   __syncthreads();
-  const double before = at_piece;
-  if (tid == 0) {
-    found = 0x7fffffff;
-    spare = -1;
-  }
-  __syncthreads();
-  // ---- the token inside the piece: thread t holds four consecutive ones
-  const int64_t row = ((int64_t)b * a.n + st.cur) * a.ld;
-  const int64_t e = (int64_t)piece * kVerifyPiece - row_shift<kBf16>(a.p, row) + 4 * tid;
-  double x[4];
-  load4<kBf16>(a.p, row, e, a.vocab, x);
-  if constexpr (kQ) {
-    const int rounds = st.rounds - (st.rounds > 0 ? undone : 0);
-    if (rounds > 0) {
-      double y[4];
-      load4<kBf16>(a.q, row, e, a.vocab, y);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = left_of(x[k], y[k], cs, rounds);
-    }
-  } else {
-    uint64_t rejected = st.rejected;
-    if (undone && st.last >= 0) rejected &= ~(1ull << st.last);
-    for (; rejected; rejected &= rejected - 1) {
-      const int64_t y = a.tokens[(int64_t)b * a.n + (int)__builtin_ctzll(rejected)];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = e + k == y ? 0.0 : x[k];
-    }
-  }
-  double all;
-  double run = before + block_scan<NW>(x[0] + x[1] + x[2] + x[3], part, &all) - (x[0] + x[1] + x[2] + x[3]);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    run += x[k];
-    if (x[k] > 0.0) {
-      if (run > goal) atomicMin(&found, (int)(e + k));
-      atomicMax(&spare, (int)(e + k));
-    }
-  }
-  __syncthreads();
-  if (tid == 0) a.next_token[b] = found != 0x7fffffff ? found : spare;
+  const int token = pick_token<kBf16, kQ>(a, b, st, cs, ws.sums + (int64_t)b * n_pieces * 2, n_pieces);
+  if (lane == 0) a.next_token[b] = token;
 }
 
 template <bool kBf16, bool kQ>
 hipError_t launch_verify(const TreeVerifyArgs& a, hipStream_t stream) {
-  const int n_pieces = (int)(((int64_t)a.vocab + 7 + kVerifyPiece - 1) / kVerifyPiece);
-  hipLaunchKernelGGL((tree_walk_kernel<kBf16, kQ>), dim3(1, (unsigned)a.batch), dim3(kWalkThreads), 0, stream, a,
-                     n_pieces);
+  const int n_pieces = tree_verify_pieces(a.vocab);
+  if (n_pieces <= kPickPieces) {
+    hipLaunchKernelGGL((tree_walk_kernel<kBf16, kQ, true>), dim3(1, (unsigned)a.batch), dim3(64 * kWalkWaves<kQ>), 0, stream, a,
+                       n_pieces);
+    return hipGetLastError();
+  }
+  // workgroups per sequence: a piece per wavefront while they fit the chip twice
+  const int most = (n_pieces + kWalkWaves<kQ> - 1) / kWalkWaves<kQ>, want = 512 / a.batch;
+  const int wgs = want < 1 ? 1 : want < most ? want : most;
+  hipLaunchKernelGGL((tree_walk_kernel<kBf16, kQ, false>), dim3((unsigned)wgs, (unsigned)a.batch), dim3(64 * kWalkWaves<kQ>), 0,
+                     stream, a, n_pieces);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((tree_pick_kernel<kBf16, kQ>), dim3((unsigned)a.batch), dim3(kPickThreads), 0, stream, a, n_pieces);
+  hipLaunchKernelGGL((tree_pick_kernel<kBf16, kQ>), dim3((unsigned)a.batch), dim3(64), 0, stream, a, n_pieces);
   return hipGetLastError();
 }
 
