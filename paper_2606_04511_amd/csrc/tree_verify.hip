@@ -152,21 +152,38 @@ __device__ __forceinline__ double wave_scan(double x) {
   return x;
 }
 
-// A lane's kPerLane weights of a piece that begins at element e0 of the row (a multiple of 4 with the row's shift),
-// after `rounds` rejections with q.
+// A lane's kPerLane weights of a piece that begins at element e0 of the row (e0 plus the row's shift is a multiple of
+// 4), after `rounds` rejections with q; *before (if given) gets their sum over the lane before the last of them.
 template <bool kBf16, bool kQ>
 __device__ __forceinline__ void piece_weights(const TreeVerifyArgs& a, int64_t row, int64_t e0, const double* c,
-                                              int rounds, double* x) {
+                                              int rounds, double* x, double* before) {
+#pragma clang fp contract(off)
   const int lane = threadIdx.x & 63;
+  auto sum = [&] {
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) s += x[k];
+    return s;
+  };
   load_piece<kBf16>(a.p, row, e0 + kPerLane * lane, a.vocab, x);
   if constexpr (kQ) {
     if (rounds > 0) {
       double y[kPerLane];
       load_piece<kBf16>(a.q, row, e0 + kPerLane * lane, a.vocab, y);
+#pragma unroll 1
+      for (int r = 0; r < rounds; ++r) {
+        if (before && r + 1 == rounds) *before = sum();
+        const double cr = c[r];
 #pragma unroll
-      for (int k = 0; k < kPerLane; ++k) x[k] = left_of(x[k], y[k], c, rounds);
+        for (int k = 0; k < kPerLane; ++k) {
+          const double cut = cr * y[k];
+          x[k] = fmax(x[k] - cut, 0.0);
+        }
+      }
+      return;
     }
   }
+  if (before) *before = sum();
 }
 
 // The next token, by one wavefront: the pieces' sums, the piece, the token.  sums: [n_pieces][2], global or LDS.
@@ -203,7 +220,7 @@ __device__ __forceinline__ int pick_token(const TreeVerifyArgs& a, int b, const 
   const int64_t row = ((int64_t)b * a.n + st.cur) * a.ld;
   const int64_t e = (int64_t)piece * kVerifyPiece - row_shift<kBf16>(a.p, row) + kPerLane * lane;
   double x[kPerLane];
-  piece_weights<kBf16, kQ>(a, row, e - kPerLane * lane, c, st.rounds - (st.rounds > 0 ? undone : 0), x);
+  piece_weights<kBf16, kQ>(a, row, e - kPerLane * lane, c, st.rounds - (st.rounds > 0 ? undone : 0), x, nullptr);
   if constexpr (!kQ) {
     uint64_t rejected = st.rejected;
     if (undone && st.last >= 0) rejected &= ~(1ull << st.last);
@@ -259,9 +276,9 @@ __global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVeri
   uint64_t kept = 1ull, rejected = 0ull;
   double c = 1.0;
   bool pending = false;  // the sum after the last rejection with q is not known yet
-  for (uint64_t rest = __ballot(cand); rest; rest &= rest - 1) {
-    const int i = (int)__builtin_ctzll(rest);
-    if (readlane_i(par, i) != cur) continue;
+  for (uint64_t kids = __ballot(cand && par == 0); kids;) {  // the untested children of cur, lowest node first
+    const int i = (int)__builtin_ctzll(kids);
+    kids &= kids - 1;
     double m = readlane_d(pv, i);
     double need = readlane_d(u, i);
     if constexpr (kQ) {
@@ -271,7 +288,7 @@ __global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVeri
         double s = 0.0;
         for (int piece = wave; piece < n_pieces; piece += NW) {
           double x[kPerLane];
-          piece_weights<kBf16, true>(a, row, (int64_t)piece * kVerifyPiece - shift, cs[wave], rounds, x);
+          piece_weights<kBf16, true>(a, row, (int64_t)piece * kVerifyPiece - shift, cs[wave], rounds, x, nullptr);
 #pragma unroll
           for (int k = 0; k < kPerLane; ++k) s += x[k];
         }
@@ -291,6 +308,7 @@ __global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVeri
     }
     if (need < m) {
       cur = i;
+      kids = __ballot(cand && par == i);
       kept |= 1ull << i;
       rounds = 0;
       last = -1;
@@ -333,20 +351,12 @@ __global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVeri
   for (int piece = blockIdx.x * NW + wave; piece < n_pieces; piece += gridDim.x * NW) {
     const int64_t e0 = (int64_t)piece * kVerifyPiece - shift;
     double x[kPerLane], s1 = 0.0, s0 = 0.0;
-    piece_weights<kBf16, kQ>(a, row, e0, cs[wave], rounds > 0 ? rounds - 1 : 0, x);
+    piece_weights<kBf16, kQ>(a, row, e0, cs[wave], rounds, x, kQ ? &s0 : nullptr);
     if constexpr (kQ) {
 #pragma unroll
-      for (int k = 0; k < kPerLane; ++k) s0 += x[k];
+      for (int k = 0; k < kPerLane; ++k) s1 += x[k];
       s0 = wave_sum(s0);
-      s1 = s0;
-      if (rounds > 0) {
-        double y[kPerLane];
-        load_piece<kBf16>(a.q, row, e0 + kPerLane * lane, a.vocab, y);
-        s1 = 0.0;
-#pragma unroll
-        for (int k = 0; k < kPerLane; ++k) s1 += left_of(x[k], y[k], cs[wave] + rounds - 1, 1);
-        s1 = wave_sum(s1);
-      }
+      s1 = wave_sum(s1);
     } else {
       if (rejected != 0ull) {  // rejected tokens of the piece weigh nothing
         if (lane < kVerifyPiece / 32) gone[wave][lane] = 0u;
