@@ -100,15 +100,15 @@ struct TreeAttnPlan {
   int32_t n_splits;
   size_t ws_bytes;
 };
-// 16-column tiles that one workgroup takes at once (1, 2 or 4).
-inline int tree_attn_tiles(int32_t n, int32_t group_size) {
+// Columns (node, query head) that one workgroup takes.
+inline int tree_attn_cols(int32_t n, int32_t group_size) {
   const int cols = n * group_size;
-  return cols <= 16 ? 1 : 2;
+  return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
 }
 // With fewer workgroups than CUs (one fits a CU) the blocks are split over them, at least half a block
 // per wavefront each.
 inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max) {
-  const int cols = n * group_size, width = 16 * tree_attn_tiles(n, group_size);
+  const int cols = n * group_size, width = tree_attn_cols(n, group_size);
   const int64_t wgs = groups * ((cols + width - 1) / width);
   const int64_t blocks = (t_max + 63) / 64 < k_total ? (t_max + 63) / 64 : k_total;
   int64_t ns = 1;

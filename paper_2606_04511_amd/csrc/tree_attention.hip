@@ -31,165 +31,92 @@ namespace sparda {
 namespace {
 
 constexpr float kLog2eT = 1.4426950408889634f;
+constexpr float kHeadroom = 8.f;                     // log2 by which a score may exceed its column's reference
 constexpr int kTaWaves = 8;
 constexpr int kTaThreads = 64 * kTaWaves;
 constexpr int kTaHalf = 32;                          // tokens per half block
 constexpr int kTaBuf = kTaHalf * kHeadDim * 2;       // bytes of a half's K or V
+constexpr int kTaSlot = 4 * kTaBuf;                  // bytes of a block's K, then its V
+constexpr int kTaRing = 4;                           // blocks in LDS at once (shared form)
 constexpr int kTaWindow = 2048;                      // blocks per window of the table
 constexpr int kTaTree = 0x7fff;                      // the list's entry of the drafted tokens
 constexpr int kTaPitch = kHeadDim + 4;               // floats per merged row: 16 rows of 16 bytes touch every bank once
+constexpr int kTaPartial = kHeadDim + 4;             // floats of a split's partial: m, l, two unused, the sums
 constexpr int kCombineThreads = 256;
 
 struct TreeAttnLds {
-  char kv[kTaWaves][2][kTaBuf];
+  char kv[kTaRing * kTaSlot];
   uint64_t table[kTaWindow];
   int16_t list[kTaWindow + 1];
   int count[kTaWaves];
 };
-static_assert(sizeof(float) * kTaWaves * 16 * (kTaPitch + 2) <= sizeof(char) * kTaWaves * 2 * kTaBuf, "a merge round fits in the buffers");
 static_assert(sizeof(TreeAttnLds) <= 160 * 1024, "LDS of one CU");
+static_assert(sizeof(float) * kTaWaves * 16 * (kTaPitch + 2) <= kTaRing * kTaSlot, "a merge round of the private form fits in the buffers");
+static_assert(sizeof(float) * 4 * 32 * (kTaPitch + 2) <= kTaRing * kTaSlot, "the merge of the shared form fits in the ring");
 
-template <int NT>
-__global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, int n_tiles, int n_groups) {
-  __shared__ __align__(16) TreeAttnLds lds;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = a.tb.n, G = a.group_size, ns = a.n_splits;
-  // workgroups 8 apart run on the same XCD: the tiles of a (group, split) share its L2
-  const int unit = (int)(blockIdx.x / (8 * n_tiles)) * 8 + (int)(blockIdx.x % 8);
-  const int tile = (int)(blockIdx.x / 8) % n_tiles;
-  if (unit >= n_groups * ns) return;
-  const int64_t bm = unit % n_groups;
-  const int split = unit / n_groups;
-  const int b = (int)(bm / a.n_kv_heads);
-  const int hh = lane & 15, grp = lane >> 4;
-  const int n_cols = n * G, c0 = tile * 16 * NT;
-  const int first_node = c0 / G, last_node = (min(c0 + 16 * NT, n_cols) - 1) / G;
-  // The tile's list entries: the first two of each thread are requested before anything is waited for.
-  const int rows = a.n_sel == 1 ? 1 : last_node - first_node + 1;
-  const int64_t row0 = a.n_sel == 1 ? bm : bm * n + first_node;
-  const int n_listed = rows * a.k_total;
-  auto list_row = [&](int e) { return e / a.k_total; };
-  auto list_entry = [&](int e) {  // the block, or -1; the count and the entry are requested together
-    const int r = list_row(e), j = a.sel[row0 * a.k_total + e], c = a.cnt[row0 + r];
-    return e - r * a.k_total < c ? j : -1;
-  };
-  constexpr int kAhead = 2;
+// What a workgroup works on: a tile of columns of one (batch, group) and a split of its blocks.
+struct TreeUnit {
+  int64_t bm;
+  int split, tile;
+  int first_node, last_node;  // of the tile
+  uint64_t anc;               // A(lane)
+  uint64_t present;           // nodes that are there
+  int t;                      // committed tokens
+};
+
+// The tile's list entries, window by window.  The first two entries of each thread are requested before
+// anything else is waited for.
+struct TreeLists {
+  static constexpr int kAhead = 2;
+  int rows, n_listed;
+  int64_t row0;
   int ahead[kAhead];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) ahead[i] = list_entry(min(tid + kTaThreads * i, n_listed - 1));
-  const int64_t ctx = tree_context(a.tb, b);
-  uint64_t anc = tree_ancestors(a.tb.parent + (int64_t)b * n, n, lane);
-  if (ctx < 0) anc = 0ull;
-  const int t = ctx < 0 ? 0 : (int)ctx;
-  const uint64_t present = __ballot(anc != 0ull);
 
-  // ---- the lane's columns (those past the last repeat it) and their queries
-  uint64_t col_anc[NT];
-  int col_node[NT];  // from the tile's first node
-  bf16x8 qb[NT][4];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int c = min(c0 + 16 * nt + hh, n_cols - 1), node = c / G;
-    col_node[nt] = node - first_node;
-    col_anc[nt] = ((uint64_t)(uint32_t)__shfl((int)(anc >> 32), node, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)anc, node, 64);
-    const uint16_t* qrow = a.q + ((bm * G + c % G) * n + node) * kHeadDim + 8 * grp;
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) qb[nt][ks] = as_bf16x8(ld16(qrow + 32 * ks));
+  __device__ __forceinline__ int entry(const TreeAttnArgs& a, int e) const {  // the block, or -1
+    const int r = e / a.k_total, j = a.sel[row0 * a.k_total + e], c = a.cnt[row0 + r];
+    return e - r * a.k_total < c ? j : -1;
   }
-  // z = zscale (q . k) with zscale > 0, so that the largest q . k has the largest z: a negative scale moves
-  // into the query's sign bits (exact), a scale of zero becomes the smallest positive one, so that masked
-  // scores (-inf) keep weight 0
-  float zscale = a.sm_scale * kLog2eT;
-  if (zscale < 0.f) {
-    zscale = -zscale;
+  __device__ __forceinline__ void request(const TreeAttnArgs& a, int64_t bm, int first_node, int last_node) {
+    rows = a.n_sel == 1 ? 1 : last_node - first_node + 1;
+    row0 = a.n_sel == 1 ? bm : bm * a.tb.n + first_node;
+    n_listed = rows * a.k_total;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        uint4 w = __builtin_bit_cast(uint4, qb[nt][ks]);
-        w.x ^= 0x80008000u;
-        w.y ^= 0x80008000u;
-        w.z ^= 0x80008000u;
-        w.w ^= 0x80008000u;
-        qb[nt][ks] = as_bf16x8(w);
-      }
-  }
-  if (zscale == 0.f) zscale = __FLT_MIN__;
-  constexpr float kHeadroom = 8.f;
-  float m_run[NT], off[NT], l_run[NT];  // off: -m_run once there is one
-  f32x4 o[NT][8];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m_run[nt] = -INFINITY;
-    off[nt] = 0.f;
-    l_run[nt] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) o[nt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < kAhead; ++i) ahead[i] = entry(a, min((int)threadIdx.x + kTaThreads * i, n_listed - 1));
   }
 
-  const char* kbuf = lds.kv[wave][0];
-  const char* vbuf = lds.kv[wave][1];
-  const uint32_t k_at = __builtin_amdgcn_readfirstlane(lds_address(kbuf));
-  const uint32_t v_at = k_at + kTaBuf;
-  // staging: instruction i brings token rows 4 i + r4; piece x of token t lies at x ^ (t % 16) for K and at
-  // x ^ 2 (t % 8) for V
-  const int r4 = lane >> 4;
-  const uint32_t k_off = r4 * 256 + 16 * ((lane & 15) ^ r4), v_off = r4 * 256 + 16 * ((lane & 15) ^ (2 * r4));
-  auto issue = [&](const uint16_t* cache, const uint16_t* drafted, int j, int hf, uint32_t off0, int flip, int by,
-                   uint32_t dst) {
-    if (j != kTaTree) {
-      const char* src = reinterpret_cast<const char*>(cache + (bm * a.t_cap + (int64_t)j * kBlock + hf * kTaHalf) * kHeadDim);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) lds_load16(src + 1024 * i, off0 ^ ((i & flip) << by), dst + 1024 * i);
-    } else {  // rows past the last node repeat it
-      const char* src = reinterpret_cast<const char*>(drafted + bm * n * kHeadDim);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = min(hf * kTaHalf + 4 * i + r4, n - 1);
-        lds_load16(src, row * 256 + ((off0 ^ ((i & flip) << by)) & 255), dst + 1024 * i);
-      }
-    }
-  };
-  auto issue_k = [&](int j, int hf) { issue(a.k, a.kt, j, hf, k_off, 3, 6, k_at); };
-  auto issue_v = [&](int j, int hf) { issue(a.v, a.vt, j, hf, v_off, 1, 7, v_at); };
-  // operand addresses: K row 16 tt + hh, piece (4 ks + grp) ^ hh; V rows 16 x + 4 grp + hh / 4, dims
-  // 16 dt + 4 (hh % 4) .. + 3
-  const uint32_t ka = hh * 256 + 16 * (grp ^ hh);
-  const int vt = 4 * grp + (hh >> 2);
-  const uint32_t va = vt * 256 + 16 * (((hh >> 1) & 1) ^ (2 * (vt & 7))) + 8 * (hh & 1);
-
-  const int nb = (t + kBlock - 1) / kBlock;
-  for (int w0 = 0; w0 == 0 || w0 < nb; w0 += kTaWindow) {
+  // The window of blocks from w0 on: table[j] = the tile's nodes that list block w0 + j, and this split's share of
+  // the blocks with a node, ascending, in list, the drafted tokens behind the last window's.  Returns the share's
+  // size; *tree_here says whether it holds the drafted tokens.  Every thread must call it.
+  __device__ __forceinline__ int window(const TreeAttnArgs& a, const TreeUnit& u, int w0, int nb, TreeAttnLds& lds,
+                                        bool* tree_here) const {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, ns = a.n_splits;
     const int wn = min(kTaWindow, nb - w0);
-    const bool final_window = w0 + kTaWindow >= nb;
-    // ---- 1. the window's table and list
     __syncthreads();  // the last window's are no longer read
     for (int i = tid; i < wn; i += kTaThreads) lds.table[i] = 0ull;
     __syncthreads();
     auto mark = [&](int e, int block) {
-      const int j = block - w0, r = list_row(e);
+      const int j = block - w0, r = e / a.k_total;
       if (block < 0 || j < 0 || j >= wn) return;
       if (a.n_sel == 1)
         lds.table[j] = ~0ull;
-      else if ((present >> (first_node + r)) & 1ull)
+      else if ((u.present >> (u.first_node + r)) & 1ull)
         atomicOr(reinterpret_cast<unsigned long long*>(&lds.table[j]), 1ull << r);
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
       if (tid + kTaThreads * i < n_listed) mark(tid + kTaThreads * i, ahead[i]);
-    for (int e = tid + kTaThreads * kAhead; e < n_listed; e += kTaThreads) mark(e, list_entry(e));
+    for (int e = tid + kTaThreads * kAhead; e < n_listed; e += kTaThreads) mark(e, entry(a, e));
     __syncthreads();
     constexpr int kRounds = kTaWindow / kTaThreads;
     uint64_t listed[kRounds];
-    int mine_n = 0;
+    int mine = 0;
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int j = (wave * kRounds + i) * 64 + lane;
       listed[i] = __ballot(j < wn && lds.table[j] != 0ull);
-      mine_n += (int)__popcll(listed[i]);
+      mine += (int)__popcll(listed[i]);
     }
-    if (lane == 0) lds.count[wave] = mine_n;
+    if (lane == 0) lds.count[wave] = mine;
     __syncthreads();
     int pos = 0, total = 0;
 #pragma unroll
@@ -200,158 +127,329 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int at = pos + mbcnt64(listed[i]);
-      if (((listed[i] >> lane) & 1ull) && at % ns == split) lds.list[at / ns] = (int16_t)((wave * kRounds + i) * 64 + lane);
+      if (((listed[i] >> lane) & 1ull) && at % ns == u.split)
+        lds.list[at / ns] = (int16_t)((wave * kRounds + i) * 64 + lane);
       pos += (int)__popcll(listed[i]);
     }
-    const bool tree_here = final_window && present != 0ull && total % ns == split;
-    const int n_entries = (total - split + ns - 1) / ns;
-    if (tree_here && tid == 0) lds.list[n_entries] = (int16_t)kTaTree;
-    const int n_items = 2 * n_entries + (tree_here ? (n > kTaHalf ? 2 : 1) : 0);
+    const int n_blocks = (total - u.split + ns - 1) / ns;
+    *tree_here = w0 + kTaWindow >= nb && u.present != 0ull && total % ns == u.split;
+    if (*tree_here && tid == 0) lds.list[n_blocks] = (int16_t)kTaTree;
     __syncthreads();
+    return n_blocks + (*tree_here ? 1 : 0);
+  }
+};
 
-    // ---- 2. and 3.
-    int jv = 0, chunk = -1;      // 64 entries of the list, one per lane
-    uint64_t mine[NT];           // which of them the column's node lists
-    auto entry = [&](int e) { return e >> 6 == chunk ? readlane_i(jv, e & 63) : __builtin_amdgcn_readfirstlane((int)lds.list[e]); };
-    auto scan = [&](int e) {
-      chunk = e >> 6;
-      const int at = chunk * 64 + lane, last = n_entries + (tree_here ? 1 : 0) - 1;
-      jv = lds.list[min(at, last)];
-      const uint64_t nodes = at <= last && jv != kTaTree ? lds.table[jv] : 0ull;
+// A wavefront's 16 NT columns: lane (hh, grp) is column hh of every tile, k-chunk and token group grp.
+template <int NT>
+struct TreeCols {
+  uint64_t anc[NT];   // A(node) of the lane's columns
+  int node[NT];       // from the tile's first node
+  bf16x8 q[NT][4];
+  float m[NT], off[NT], l[NT];  // the softmax reference, -m once there is one (else 0), the lane's sum
+  f32x4 o[NT][8];               // dims 16 dt + 4 grp + e
+  float zscale;
+  // 64 entries of the list, one per lane, and which of them each column's node lists
+  int jv, chunk;
+  uint64_t mine[NT];
+
+  // Columns c0 + 16 nt + hh (those past n_cols repeat the last).
+  __device__ __forceinline__ void load(const TreeAttnArgs& a, const TreeUnit& u, int c0) {
+    const int lane = threadIdx.x & 63, hh = lane & 15, grp = lane >> 4, n = a.tb.n, G = a.group_size;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int c = min(c0 + 16 * nt + hh, n * G - 1), x = c / G;
+      node[nt] = x - u.first_node;
+      anc[nt] = ((uint64_t)(uint32_t)__shfl((int)(u.anc >> 32), x, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)u.anc, x, 64);
+      const uint16_t* qrow = a.q + ((u.bm * G + c % G) * n + x) * kHeadDim + 8 * grp;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) q[nt][ks] = as_bf16x8(ld16(qrow + 32 * ks));
+      m[nt] = -INFINITY;
+      off[nt] = l[nt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) o[nt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // z = zscale (q . k) with zscale > 0, so that the largest q . k has the largest z: a negative scale moves into the
+    // query's sign bits (exact), a scale of zero becomes the smallest positive one, so that masked scores (-inf) keep
+    // weight 0
+    zscale = a.sm_scale * kLog2eT;
+    if (zscale < 0.f) {
+      zscale = -zscale;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          uint4 w = __builtin_bit_cast(uint4, q[nt][ks]);
+          w.x ^= 0x80008000u;
+          w.y ^= 0x80008000u;
+          w.z ^= 0x80008000u;
+          w.w ^= 0x80008000u;
+          q[nt][ks] = as_bf16x8(w);
+        }
+    }
+    if (zscale == 0.f) zscale = __FLT_MIN__;
+  }
+
+  // Entry e of the list: the block from the window's first on, or kTaTree.
+  __device__ __forceinline__ int entry(const TreeAttnLds& lds, int e) const {
+    return e >> 6 == chunk ? readlane_i(jv, e & 63) : __builtin_amdgcn_readfirstlane((int)lds.list[e]);
+  }
+  // Takes up the 64 entries around e of n_list.
+  __device__ __forceinline__ void scan(const TreeAttnArgs& a, const TreeAttnLds& lds, int e, int n_list) {
+    const int lane = threadIdx.x & 63;
+    chunk = e >> 6;
+    const int at = chunk * 64 + lane;
+    jv = lds.list[min(at, n_list - 1)];
+    const uint64_t nodes = at < n_list && jv != kTaTree ? lds.table[jv] : 0ull;
+    if (a.n_sel == 1) {
+      const uint64_t x = __ballot(nodes != 0ull);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mine[nt] = anc[nt] ? x : 0ull;
+    } else {
+      const int lo = readlane_i(node[0], 0), hi = readlane_i(node[NT - 1], 15);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mine[nt] = 0ull;
-      if (a.n_sel == 1) {
-        const uint64_t x = __ballot(nodes != 0ull);
+      for (int r = lo; r <= hi; ++r) {
+        const uint64_t x = __ballot(((nodes >> r) & 1ull) != 0ull);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mine[nt] = col_anc[nt] ? x : 0ull;
-      } else {
-        for (int r = 0; r <= last_node - first_node; ++r) {
-          const uint64_t x = __ballot(((nodes >> r) & 1ull) != 0ull);
+        for (int nt = 0; nt < NT; ++nt) mine[nt] = node[nt] == r ? x : mine[nt];
+      }
+    }
+  }
+
+  // One half block: K rows at kbuf, V rows at vbuf (rows of 256 bytes, 16-byte piece x of token t at x ^ (t % 16) for K
+  // and x ^ 2 (t % 8) for V).  valid: its tokens that hold a V; they are the context's, or the drafted ones from node
+  // 32 hf on.  k_read runs once K has been read, v_ready before V is, v_read after.
+  template <class KRead, class VReady>
+  __device__ __forceinline__ void half(const char* kbuf, const char* vbuf, bool tree, int hf, int e, uint32_t valid,
+                                       KRead k_read, VReady v_ready) {
+    const int lane = threadIdx.x & 63, hh = lane & 15, grp = lane >> 4;
+    // operand addresses: K row 16 tt + hh, piece (4 ks + grp) ^ hh; V rows 16 x + 4 grp + hh / 4, dims
+    // 16 dt + 4 (hh % 4) .. + 3
+    const uint32_t ka = hh * 256 + 16 * (grp ^ hh);
+    const int vt = 4 * grp + (hh >> 2);
+    const uint32_t va = vt * 256 + 16 * (((hh >> 1) & 1) ^ (2 * (vt & 7))) + 8 * (hh & 1);
+    uint32_t vis[NT];
+    bool on[NT], part[NT];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mine[nt] = col_node[nt] == r ? x : mine[nt];
+    for (int nt = 0; nt < NT; ++nt) {
+      vis[nt] = tree ? (uint32_t)(anc[nt] >> (hf * kTaHalf)) : (mine[nt] >> (e & 63)) & 1ull ? valid : 0u;
+      on[nt] = __ballot(vis[nt] != 0u) != 0ull;
+      part[nt] = __ballot(vis[nt] != ~0u) != 0ull;
+    }
+    bf16x8 kf[2][4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+        kf[tt][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(kbuf + 4096 * tt + (ka ^ (ks << 6))));
+    f32x4 st[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      st[nt][0] = st[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (!on[nt]) continue;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) st[nt][tt] = mfma16x16x32(kf[tt][ks], q[nt][ks], st[nt][tt]);
+    }
+    k_read();
+    float top[NT];
+    bool ask = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      top[nt] = -INFINITY;
+      if (!on[nt]) continue;
+      if (part[nt]) {
+        const uint32_t bits = vis[nt] >> (4 * grp);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st[nt][tt][i] = (bits >> (16 * tt + i)) & 1u ? st[nt][tt][i] : -INFINITY;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+        top[nt] = fmaxf(top[nt], fmaxf(fmaxf(st[nt][tt][0], st[nt][tt][1]), fmaxf(st[nt][tt][2], st[nt][tt][3])));
+      top[nt] *= zscale;
+      ask |= top[nt] > m[nt] + kHeadroom;  // also on a column's first scores
+    }
+    if (__ballot(ask) != 0ull) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x = top[nt];
+        x = fmaxf(x, __shfl_xor(x, 16, 64));
+        x = fmaxf(x, __shfl_xor(x, 32, 64));
+        if (x > m[nt] + kHeadroom) {
+          const float alpha = __builtin_amdgcn_exp2f(m[nt] - x);
+          m[nt] = x;
+          off[nt] = -x;
+          l[nt] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < 8; ++dt) o[nt][dt] *= alpha;
         }
       }
-    };
+    }
+    bf16x8 pb[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (!on[nt]) continue;
+      float p[2][4];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[tt][i] = __builtin_amdgcn_exp2f(fmaf(st[nt][tt][i], zscale, off[nt]));
+          l[nt] += p[tt][i];
+        }
+      pb[nt] = as_bf16x8(make_uint4(pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]),
+                                    pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])));
+    }
+    v_ready();
+    bf16x8 vf[8];
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+      const uint2 v0 = lds_read_tr16(vbuf + (va ^ (dt << 5))), v1 = lds_read_tr16(vbuf + 4096 + (va ^ (dt << 5)));
+      vf[dt] = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (!on[nt]) continue;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) o[nt][dt] = mfma16x16x32(vf[dt], pb[nt], o[nt][dt]);
+    }
+  }
+
+  __device__ __forceinline__ float row_sum(int nt) const {  // l over the column's four lanes
+    float x = l[nt];
+    x += __shfl_xor(x, 16, 64);
+    x += __shfl_xor(x, 32, 64);
+    return x;
+  }
+};
+
+// The tokens of a half block that hold a V.
+__device__ __forceinline__ uint32_t half_valid(const TreeUnit& u, bool tree, int j, int hf) {
+  if (tree) return (uint32_t)(u.present >> (hf * kTaHalf));
+  const int left = u.t - (j * kBlock + hf * kTaHalf);  // committed tokens from the half's first on
+  return left >= kTaHalf ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+}
+
+// Four dims of a finished column, or of a split's partial.
+__device__ __forceinline__ void store_dims(const TreeAttnArgs& a, const TreeUnit& u, int c, int d, float m, float den,
+                                           f32x4 num) {
+  const int64_t row = (u.bm * a.group_size + c % a.group_size) * a.tb.n + c / a.group_size;
+  if (a.n_splits == 1) {
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    uint2 w;
+    w.x = (uint32_t)f32_to_bf16(num[0] * inv) | ((uint32_t)f32_to_bf16(num[1] * inv) << 16);
+    w.y = (uint32_t)f32_to_bf16(num[2] * inv) | ((uint32_t)f32_to_bf16(num[3] * inv) << 16);
+    *reinterpret_cast<uint2*>(a.o + row * kHeadDim + d) = w;
+  } else {
+    float* pp = a.ws + (row * a.n_splits + u.split) * kTaPartial;
+    if (d == 0) *reinterpret_cast<float2*>(pp) = make_float2(m, den);
+    *reinterpret_cast<f32x4*>(pp + 4 + d) = num;
+  }
+}
+
+// The workgroup's unit; false: none.  Workgroups 8 apart run on the same XCD: the tiles of a (group, split) share its L2.
+__device__ __forceinline__ bool tree_unit(const TreeAttnArgs& a, int n_tiles, int n_groups, int tile_cols,
+                                          TreeUnit* u, TreeLists* lists) {
+  const int lane = threadIdx.x & 63, n = a.tb.n, G = a.group_size;
+  const int unit = (int)(blockIdx.x / (8 * n_tiles)) * 8 + (int)(blockIdx.x % 8);
+  if (unit >= n_groups * a.n_splits) return false;
+  u->tile = (int)(blockIdx.x / 8) % n_tiles;
+  u->bm = unit % n_groups;
+  u->split = unit / n_groups;
+  const int c0 = u->tile * tile_cols;
+  u->first_node = c0 / G;
+  u->last_node = (min(c0 + tile_cols, n * G) - 1) / G;
+  lists->request(a, u->bm, u->first_node, u->last_node);
+  const int b = (int)(u->bm / a.n_kv_heads);
+  const int64_t ctx = tree_context(a.tb, b);
+  u->anc = tree_ancestors(a.tb.parent + (int64_t)b * n, n, lane);
+  if (ctx < 0) u->anc = 0ull;
+  u->t = ctx < 0 ? 0 : (int)ctx;
+  u->present = __ballot(u->anc != 0ull);
+  return true;
+}
+
+// ---- up to 32 columns: every wavefront streams halves of its own -------------------------------------
+
+template <int NT>
+__global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, int n_tiles, int n_groups) {
+  __shared__ __align__(16) TreeAttnLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = a.tb.n, c0_tile = 16 * NT;
+  TreeUnit u;
+  TreeLists lists;
+  if (!tree_unit(a, n_tiles, n_groups, c0_tile, &u, &lists)) return;
+  const int c0 = u.tile * c0_tile;
+  TreeCols<NT> cols;
+  cols.load(a, u, c0);
+
+  char* const kbuf = lds.kv + wave * 2 * kTaBuf;
+  char* const vbuf = kbuf + kTaBuf;
+  const uint32_t k_at = __builtin_amdgcn_readfirstlane(lds_address(kbuf)), v_at = k_at + kTaBuf;
+  // staging: instruction i brings token rows 4 i + r4
+  const int r4 = lane >> 4;
+  const uint32_t k_off = r4 * 256 + 16 * ((lane & 15) ^ r4), v_off = r4 * 256 + 16 * ((lane & 15) ^ (2 * r4));
+  auto issue = [&](const uint16_t* cache, const uint16_t* drafted, int j, int hf, uint32_t off0, int flip, int by,
+                   uint32_t dst) {
+    if (j != kTaTree) {
+      const char* src = reinterpret_cast<const char*>(cache + (u.bm * a.t_cap + (int64_t)j * kBlock + hf * kTaHalf) * kHeadDim);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lds_load16(src + 1024 * i, off0 ^ ((i & flip) << by), dst + 1024 * i);
+    } else {  // rows past the last node repeat it
+      const char* src = reinterpret_cast<const char*>(drafted + u.bm * n * kHeadDim);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = min(hf * kTaHalf + 4 * i + r4, n - 1);
+        lds_load16(src, row * 256 + ((off0 ^ ((i & flip) << by)) & 255), dst + 1024 * i);
+      }
+    }
+  };
+  auto issue_k = [&](int j, int hf) { issue(a.k, a.kt, j, hf, k_off, 3, 6, k_at); };
+  auto issue_v = [&](int j, int hf) { issue(a.v, a.vt, j, hf, v_off, 1, 7, v_at); };
+
+  const int nb = (u.t + kBlock - 1) / kBlock;
+  for (int w0 = 0; w0 == 0 || w0 < nb; w0 += kTaWindow) {
+    bool tree_here;
+    const int n_list = lists.window(a, u, w0, nb, lds, &tree_here);
+    const int n_items = 2 * n_list - (tree_here && n <= kTaHalf ? 1 : 0);
     auto block_of = [&](int j) { return j == kTaTree ? j : j + w0; };
+    cols.chunk = -1;
     int x = wave;
     int j = 0;
     if (x < n_items) {
-      j = block_of(entry(x >> 1));
+      j = block_of(cols.entry(lds, x >> 1));
       issue_k(j, x & 1);
       issue_v(j, x & 1);
     }
     lds_loads_landed();  // the first half and the queries: from here on the loads are counted
     while (x < n_items) {
       const int e = x >> 1, hf = x & 1, x2 = x + kTaWaves;
-      const bool more = x2 < n_items;
-      if (e >> 6 != chunk) scan(e);
-      const int j2 = more ? block_of(entry(x2 >> 1)) : 0;
-      // which tokens of the half hold a V, and which of them each column sees
-      const bool tree = j == kTaTree;
-      const int left = t - (j * kBlock + hf * kTaHalf);  // committed tokens from the half's first on
-      const uint32_t valid = tree ? (uint32_t)(present >> (hf * kTaHalf)) : left >= kTaHalf ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
-      uint32_t vis[NT];
-      bool on[NT], part[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        vis[nt] = tree ? (uint32_t)(col_anc[nt] >> (hf * kTaHalf)) : (mine[nt] >> (e & 63)) & 1ull ? valid : 0u;
-        on[nt] = __ballot(vis[nt] != 0u) != 0ull;
-        part[nt] = __ballot(vis[nt] != ~0u) != 0ull;
-      }
+      const bool more = x2 < n_items, tree = j == kTaTree;
+      if (e >> 6 != cols.chunk) cols.scan(a, lds, e, n_list);
+      const int j2 = more ? block_of(cols.entry(lds, x2 >> 1)) : 0;
+      const uint32_t valid = half_valid(u, tree, j, hf);
       __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");  // this half's K (its V may be under way)
-      bf16x8 kf[2][4];
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-          kf[tt][ks] = as_bf16x8(*reinterpret_cast<const uint4*>(kbuf + 4096 * tt + (ka ^ (ks << 6))));
-      f32x4 st[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        st[nt][0] = st[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (!on[nt]) continue;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) st[nt][tt] = mfma16x16x32(kf[tt][ks], qb[nt][ks], st[nt][tt]);
-      }
-      __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
-      if (more) issue_k(j2, x2 & 1);
-      float bmax[NT];
-      bool ask = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (!on[nt]) {
-          bmax[nt] = -INFINITY;
-          continue;
-        }
-        if (part[nt]) {
-          const uint32_t bits = vis[nt] >> (4 * grp);
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) st[nt][tt][i] = (bits >> (16 * tt + i)) & 1u ? st[nt][tt][i] : -INFINITY;
-        }
-        float top = -INFINITY;
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-          top = fmaxf(top, fmaxf(fmaxf(st[nt][tt][0], st[nt][tt][1]), fmaxf(st[nt][tt][2], st[nt][tt][3])));
-        bmax[nt] = top * zscale;
-        ask |= bmax[nt] > m_run[nt] + kHeadroom;  // also on a column's first scores
-      }
-      if (__ballot(ask) != 0ull) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float m = bmax[nt];
-          m = fmaxf(m, __shfl_xor(m, 16, 64));
-          m = fmaxf(m, __shfl_xor(m, 32, 64));
-          if (m > m_run[nt] + kHeadroom) {
-            const float alpha = __builtin_amdgcn_exp2f(m_run[nt] - m);
-            m_run[nt] = m;
-            off[nt] = -m;
-            l_run[nt] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) o[nt][dt] *= alpha;
-          }
-        }
-      }
-      bf16x8 pb[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (!on[nt]) continue;
-        float p[2][4];
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[tt][i] = __builtin_amdgcn_exp2f(fmaf(st[nt][tt][i], zscale, off[nt]));
-            l_run[nt] += p[tt][i];
-          }
-        pb[nt] = as_bf16x8(make_uint4(pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]),
-                                      pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])));
-      }
-      if (more)
-        __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");  // this half's V (the next K may be under way)
-      else
-        __asm__ __volatile__("s_waitcnt vmcnt(0)" ::: "memory");
-      if (valid != ~0u) {  // rows that no column may see: whatever lies there becomes zeros
-        for (int r = r4; r < kTaHalf; r += 4)
-          if (!((valid >> r) & 1u))
-            *reinterpret_cast<uint4*>(&lds.kv[wave][1][r * 256 + 16 * (lane & 15)]) = make_uint4(0u, 0u, 0u, 0u);
-        wave_lds_sync();
-      }
-      bf16x8 vf[8];
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const uint2 v0 = lds_read_tr16(vbuf + (va ^ (dt << 5))), v1 = lds_read_tr16(vbuf + 4096 + (va ^ (dt << 5)));
-        vf[dt] = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (!on[nt]) continue;
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) o[nt][dt] = mfma16x16x32(vf[dt], pb[nt], o[nt][dt]);
-      }
+      cols.half(
+          kbuf, vbuf, tree, hf, e, valid,
+          [&] {
+            __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
+            if (more) issue_k(j2, x2 & 1);
+          },
+          [&] {
+            if (more)
+              __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");  // this half's V (the next K may be under way)
+            else
+              __asm__ __volatile__("s_waitcnt vmcnt(0)" ::: "memory");
+            if (valid != ~0u) {  // rows that no column may see: whatever lies there becomes zeros
+              for (int r = r4; r < kTaHalf; r += 4)
+                if (!((valid >> r) & 1u)) *reinterpret_cast<uint4*>(vbuf + r * 256 + 16 * (lane & 15)) = make_uint4(0u, 0u, 0u, 0u);
+              wave_lds_sync();
+            }
+          });
       __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
       if (more) issue_v(j2, x2 & 1);
       x = x2;
@@ -359,26 +457,24 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
     }
   }
 
-  // ---- 4. the wavefronts' states, 16 columns at a time, through the buffers' space
-  float* st_m = reinterpret_cast<float*>(&lds.kv[0][0][0]);  // [waves][16]
-  float* st_l = st_m + kTaWaves * 16;                        // [waves][16]
-  float* st_o = st_l + kTaWaves * 16;                        // [waves][16][kTaPitch]
+  // the wavefronts' states, 16 columns at a time, through the buffers' space
+  float* st_m = reinterpret_cast<float*>(lds.kv);  // [waves][16]
+  float* st_l = st_m + kTaWaves * 16;              // [waves][16]
+  float* st_o = st_l + kTaWaves * 16;              // [waves][16][kTaPitch]
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     __syncthreads();
-    float l = l_run[nt];
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    const float l = cols.row_sum(nt);
     if (grp == 0) {
-      st_m[wave * 16 + hh] = m_run[nt];
+      st_m[wave * 16 + hh] = cols.m[nt];
       st_l[wave * 16 + hh] = l;
     }
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt)
-      *reinterpret_cast<f32x4*>(&st_o[(wave * 16 + hh) * kTaPitch + 16 * dt + 4 * grp]) = o[nt][dt];
+      *reinterpret_cast<f32x4*>(&st_o[(wave * 16 + hh) * kTaPitch + 16 * dt + 4 * grp]) = cols.o[nt][dt];
     __syncthreads();
     const int cl = tid >> 5, d = 4 * (tid & 31), c = c0 + 16 * nt + cl;  // 16 columns x 32 quads of dims
-    if (c < n_cols) {
+    if (c < n * a.group_size) {
       float m = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kTaWaves; ++w) m = fmaxf(m, st_m[w * 16 + cl]);
@@ -392,19 +488,132 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
           num += *reinterpret_cast<const f32x4*>(&st_o[(w * 16 + cl) * kTaPitch + d]) * sc;
         }
       }
-      const int64_t row = (bm * G + c % G) * n + c / G;
-      if (ns == 1) {
-        const float inv = den > 0.f ? 1.f / den : 0.f;
-        uint2 w;
-        w.x = (uint32_t)f32_to_bf16(num[0] * inv) | ((uint32_t)f32_to_bf16(num[1] * inv) << 16);
-        w.y = (uint32_t)f32_to_bf16(num[2] * inv) | ((uint32_t)f32_to_bf16(num[3] * inv) << 16);
-        *reinterpret_cast<uint2*>(a.o + row * kHeadDim + d) = w;
-      } else {
-        float* pp = a.ws + (row * ns + split) * (kHeadDim + 4);
-        if (d == 0) *reinterpret_cast<float2*>(pp) = make_float2(m, den);
-        *reinterpret_cast<f32x4*>(pp + 4 + d) = num;
+      store_dims(a, u, c, d, m, den, num);
+    }
+  }
+}
+
+// ---- more columns: the wavefronts share the blocks ------------------------------------------------------
+
+// WC groups of 16 NT columns; with WC = 4 two wavefronts take a group, one half of every block each.
+template <int NT, int WC>
+__global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnArgs a, int n_tiles, int n_groups) {
+  constexpr int WT = kTaWaves / WC;
+  static_assert(WT == 1 || WT == 2, "a wavefront takes whole blocks or halves");
+  __shared__ __align__(16) TreeAttnLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cg = wave % WC, th = wave / WC;
+  const int n = a.tb.n;
+  TreeUnit u;
+  TreeLists lists;
+  if (!tree_unit(a, n_tiles, n_groups, 16 * NT * WC, &u, &lists)) return;
+  const int c0 = (u.tile * WC + cg) * 16 * NT;
+  const bool live = c0 < n * a.group_size;  // the last tile may leave wavefronts without columns: they only load
+  TreeCols<NT> cols;
+  cols.load(a, u, c0);
+
+  // staging: a wavefront brings token rows 8 wave .. + 7 of K and of V, 4 rows per instruction
+  const int r4 = lane >> 4;
+  const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(lds.kv)) + wave * 2048;
+  auto issue = [&](int j, int slot) {
+    const uint32_t dst = ring_at + slot * kTaSlot;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 8 * wave + 4 * i + r4;
+      const uint32_t kx = 16 * ((lane & 15) ^ (row & 15)), vx = 16 * ((lane & 15) ^ (2 * (row & 7)));
+      if (j != kTaTree) {
+        const int64_t at = (u.bm * a.t_cap + (int64_t)j * kBlock) * kHeadDim;
+        lds_load16(a.k + at, row * 256 + kx, dst + 1024 * i);
+        lds_load16(a.v + at, row * 256 + vx, dst + 2 * kTaBuf + 1024 * i);
+      } else {  // rows past the last node repeat it
+        const int64_t at = u.bm * n * kHeadDim;
+        lds_load16(a.kt + at, min(row, n - 1) * 256 + kx, dst + 1024 * i);
+        lds_load16(a.vt + at, min(row, n - 1) * 256 + vx, dst + 2 * kTaBuf + 1024 * i);
       }
     }
+  };
+
+  const int nb = (u.t + kBlock - 1) / kBlock;
+  for (int w0 = 0; w0 == 0 || w0 < nb; w0 += kTaWindow) {
+    bool tree_here;
+    const int n_list = lists.window(a, u, w0, nb, lds, &tree_here);
+    auto block_of = [&](int j) { return j == kTaTree ? j : j + w0; };
+    cols.chunk = -1;
+    lds_loads_landed();  // the queries: from here on the loads are counted, 4 per block
+#pragma unroll
+    for (int s = 0; s < kTaRing - 1; ++s)
+      if (s < n_list) issue(block_of(cols.entry(lds, s)), s);
+    for (int s = 0; s < n_list; ++s) {
+      if (s >> 6 != cols.chunk) cols.scan(a, lds, s, n_list);
+      const int j = block_of(cols.entry(lds, s));
+      const bool tree = j == kTaTree;
+      char* const kslot = lds.kv + (s % kTaRing) * kTaSlot;
+      char* const vslot = kslot + 2 * kTaBuf;
+      // this wavefront's rows of block s have landed (two more blocks may be under way), the rows of V that no column
+      // may see become zeros, and its reads of block s - 1 have returned; then everybody's have
+      if (s + 2 < n_list)
+        __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");
+      else if (s + 1 < n_list)
+        __asm__ __volatile__("s_waitcnt vmcnt(4)" ::: "memory");
+      else
+        __asm__ __volatile__("s_waitcnt vmcnt(0)" ::: "memory");
+      const uint32_t valid[2] = {half_valid(u, tree, j, 0), half_valid(u, tree, j, 1)};
+      if ((valid[0] & valid[1]) != ~0u) {
+        for (int r = 8 * wave + r4; r < 8 * wave + 8; r += 4)
+          if (!((valid[r >> 5] >> (r & 31)) & 1u)) *reinterpret_cast<uint4*>(vslot + r * 256 + 16 * (lane & 15)) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      __asm__ __volatile__("" ::: "memory");
+      if (s + kTaRing - 1 < n_list) issue(block_of(cols.entry(lds, s + kTaRing - 1)), (s + kTaRing - 1) % kTaRing);
+      if (!live) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (WT == 2 && h != th) continue;
+        cols.half(kslot + h * kTaBuf, vslot + h * kTaBuf, tree, h, s, valid[h], [] {}, [] {});
+      }
+    }
+    __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+
+  if constexpr (WT == 2) {  // the second half's states, through the ring's space
+    __syncthreads();
+    float* st_m = reinterpret_cast<float*>(lds.kv);  // [WC][16 NT]
+    float* st_l = st_m + WC * 16 * NT;
+    float* st_o = st_l + WC * 16 * NT;               // [WC][16 NT][kTaPitch]
+    const int at = cg * 16 * NT + hh;
+    if (th == 1) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        if (grp == 0) st_m[at + 16 * nt] = cols.m[nt];
+        const float l = cols.row_sum(nt);
+        if (grp == 0) st_l[at + 16 * nt] = l;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+          *reinterpret_cast<f32x4*>(&st_o[(at + 16 * nt) * kTaPitch + 16 * dt + 4 * grp]) = cols.o[nt][dt];
+      }
+    }
+    __syncthreads();
+    if (th == 1) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float m1 = st_m[at + 16 * nt], m = fmaxf(cols.m[nt], m1), ref = m > -INFINITY ? m : 0.f;
+      const float s0 = __builtin_amdgcn_exp2f(cols.m[nt] - ref), s1 = __builtin_amdgcn_exp2f(m1 - ref);
+      cols.l[nt] = cols.row_sum(nt) * s0 + st_l[at + 16 * nt] * s1;
+      cols.m[nt] = m;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt)
+        cols.o[nt][dt] = cols.o[nt][dt] * s0 + *reinterpret_cast<const f32x4*>(&st_o[(at + 16 * nt) * kTaPitch + 16 * dt + 4 * grp]) * s1;
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float l = WT == 2 ? cols.l[nt] : cols.row_sum(nt);
+    const int c = c0 + 16 * nt + hh;
+    if (c >= n * a.group_size) continue;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) store_dims(a, u, c, 16 * dt + 4 * grp, cols.m[nt], l, cols.o[nt][dt]);
   }
 }
 
@@ -414,7 +623,7 @@ __global__ __launch_bounds__(kCombineThreads) void tree_combine_kernel(TreeAttnA
   const int lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * (kCombineThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= n_rows) return;
-  constexpr int kStride = kHeadDim + 4;
+  constexpr int kStride = kTaPartial;
   const float* base = a.ws + row * a.n_splits * kStride;
   float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
   for (int s0 = 0; s0 < a.n_splits; s0 += 8) {
@@ -448,22 +657,24 @@ __global__ __launch_bounds__(kCombineThreads) void tree_combine_kernel(TreeAttnA
   reinterpret_cast<uint32_t*>(a.o + row * kHeadDim)[lane] = (uint32_t)f32_to_bf16(o0 * inv) | ((uint32_t)f32_to_bf16(o1 * inv) << 16);
 }
 
-template <int NT>
-hipError_t launch_tiles(const TreeAttnArgs& a, hipStream_t stream) {
+template <class Kernel>
+hipError_t launch_tiles(Kernel kernel, const TreeAttnArgs& a, int tile_cols, hipStream_t stream) {
   const int groups = a.tb.batch * a.n_kv_heads, units = groups * a.n_splits;
-  const int n_tiles = (a.tb.n * a.group_size + 16 * NT - 1) / (16 * NT);
-  hipLaunchKernelGGL(tree_attn_kernel<NT>, dim3((unsigned)((units + 7) / 8 * 8 * n_tiles)), dim3(kTaThreads), 0, stream, a,
-                     n_tiles, groups);
+  const int n_tiles = (a.tb.n * a.group_size + tile_cols - 1) / tile_cols;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((units + 7) / 8 * 8 * n_tiles)), dim3(kTaThreads), 0, stream, a, n_tiles,
+                     groups);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t stream) {
-  const int nt = tree_attn_tiles(a.tb.n, a.group_size);
-  const hipError_t e = nt == 1   ? launch_tiles<1>(a, stream)
-                       : nt == 2 ? launch_tiles<2>(a, stream)
-                                 : launch_tiles<4>(a, stream);
+  const int cols = tree_attn_cols(a.tb.n, a.group_size);
+  const hipError_t e = cols == 16    ? launch_tiles(tree_attn_kernel<1>, a, cols, stream)
+                       : cols == 32  ? launch_tiles(tree_attn_kernel<2>, a, cols, stream)
+                       : cols == 64  ? launch_tiles(tree_attn_shared_kernel<1, 4>, a, cols, stream)
+                       : cols == 128 ? launch_tiles(tree_attn_shared_kernel<2, 4>, a, cols, stream)
+                                     : launch_tiles(tree_attn_shared_kernel<2, 8>, a, cols, stream);
   if (e != hipSuccess || a.n_splits == 1) return e;
   const int64_t rows = (int64_t)a.tb.batch * a.n_kv_heads * a.group_size * a.tb.n;
   hipLaunchKernelGGL(tree_combine_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(kCombineThreads), 0, stream, a, rows);

@@ -154,9 +154,17 @@ def _p(x):
     return x.data_ptr()
 
 
+# The current stream's handle without a Stream object around it (0.4 us instead of 2.9 us per call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
+        if not torch.cuda.is_available():
+            return 0
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
