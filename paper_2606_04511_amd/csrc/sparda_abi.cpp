@@ -260,7 +260,7 @@ int sparda_workspace_size(const sparda_shape* shape, int32_t op, int32_t n_q, in
     if (op == SPARDA_OP_TREE_SELECT)
       *bytes = sparda::tree_select_ws(groups, q_pos0, n_q, shape->n_init, shape->n_local);
     else
-      *bytes = sparda::tree_attn_plan(groups, n_q, shape->group_size, shape->k_total, q_pos0).ws_bytes;
+      *bytes = sparda::tree_attn_ws(groups, n_q, shape->group_size, shape->k_total, q_pos0);
   } else {
     return fail(SPARDA_ERR_INVALID_ARG, "unknown op %d", op);
   }

@@ -51,7 +51,10 @@ struct TreeAttnArgs {
   int32_t n_kv_heads, group_size, n_sel, k_total;
   int64_t t_cap;
   float sm_scale;
-  int32_t n_splits;
+  int32_t width, n_splits;  // the plan
+  uint64_t k_recip;    // ceil(2^36 / k_total)
+  uint32_t ns_recip;   // ceil(2^20 / n_splits)
+  uint32_t g_recip;    // ceil(2^16 / group_size)
 };
 
 struct TreeVerifyArgs {
@@ -95,30 +98,50 @@ inline size_t tree_select_ws(int64_t groups, int64_t t_max, int32_t n, int32_t n
   return (size_t)groups * n * (size_t)tree_select_stride(t_max, n, n_init, n_local) * sizeof(float);
 }
 
-// Splits of a (batch, group)'s blocks and the bytes of their partials.
+// How an attention call is cut into workgroups, one of which fits a CU.
 struct TreeAttnPlan {
-  int32_t n_splits;
-  size_t ws_bytes;
+  int32_t width;     // columns (node, query head) of a workgroup: 16 or 32, whose wavefronts stream blocks of
+                     // their own, or 64, 128 or 256, whose wavefronts share them
+  int32_t n_splits;  // of a (batch, group)'s blocks
+  size_t ws_bytes;   // partials of the splits
 };
-// Columns (node, query head) that one workgroup takes.
-inline int tree_attn_cols(int32_t n, int32_t group_size) {
+
+// Above 32 columns, narrow tiles read a block once for every 32 columns, wide ones once for up to 256 but then all
+// wavefronts of a workgroup wait for each other at every block.  While the blocks of all groups fit the 256 MB
+// last-level cache the narrow ones win, beyond it the wide ones.  Measured (us), 32 columns against the widest, at 32K
+// with 64 blocks per list: one list per node (about 150 blocks in all): 32 and 64 nodes of 32 groups of 4 heads 57 and
+// 62, 78 and 98; 24 and 32 nodes of 64 groups 102 and 85, 115 and 94; of 128 groups 217 and 165 (32 nodes); 64 nodes of
+// 16 groups of 16 heads 78 and 108.  One list for all: 16 nodes of 64 groups 32 and 35, of 128 groups 49 and 57 (64
+// nodes 144 and 114), of 256 groups 110 and 94.
+// With fewer workgroups than CUs the blocks are split over them: at least half a block per wavefront, or three blocks
+// per workgroup where the wavefronts share them (one each: 19 -> 24 us for 22 nodes of 3 groups of 4 heads, 55 blocks).
+inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max,
+                                   bool one_list) {
+  TreeAttnPlan p;
   const int cols = n * group_size;
-  return cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  const int64_t most_blocks = (t_max + 63) / 64;
+  auto at_most = [&](int64_t x) { return most_blocks < x ? most_blocks : x; };
+  const int64_t bytes = groups * at_most((int64_t)k_total * (one_list || n == 1 ? 1 : 2)) * (2 * 64 * 128 * 2);
+  if (cols <= 16)
+    p.width = 16;
+  else if (cols <= 32 || bytes < ((int64_t)256 << 20))
+    p.width = 32;
+  else
+    p.width = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  const int64_t wgs = groups * ((cols + p.width - 1) / p.width), blocks = at_most(k_total);
+  int64_t ns = 256 / wgs;
+  const int64_t most = p.width <= 32 ? (2 * blocks + 2 + 7) / 8 : (blocks + 1 + 2) / 3;
+  ns = ns < most ? ns : most;
+  ns = ns > 64 ? 64 : ns < 1 ? 1 : ns;
+  p.n_splits = (int32_t)ns;
+  p.ws_bytes = ns == 1 ? 0 : (size_t)groups * cols * (size_t)ns * (128 + 4) * sizeof(float);
+  return p;
 }
-// With fewer workgroups than CUs (one fits a CU) the blocks are split over them, at least half a block
-// per wavefront each.
-inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max) {
-  const int cols = n * group_size, width = tree_attn_cols(n, group_size);
-  const int64_t wgs = groups * ((cols + width - 1) / width);
-  const int64_t blocks = (t_max + 63) / 64 < k_total ? (t_max + 63) / 64 : k_total;
-  int64_t ns = 1;
-  if (wgs < 256) {
-    const int64_t want = (256 + wgs - 1) / wgs, most = (2 * blocks + 2 + 7) / 8;
-    ns = want < most ? want : most;
-    if (ns > 64) ns = 64;
-  }
-  const size_t bytes = ns == 1 ? 0 : (size_t)groups * cols * (size_t)ns * (128 + 4) * sizeof(float);
-  return {(int32_t)ns, bytes};
+// The workspace covers both kinds of lists.
+inline size_t tree_attn_ws(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max) {
+  const size_t a = tree_attn_plan(groups, n, group_size, k_total, t_max, true).ws_bytes;
+  const size_t b = tree_attn_plan(groups, n, group_size, k_total, t_max, false).ws_bytes;
+  return a > b ? a : b;
 }
 
 // Workspace of the verification: per sequence the state that the walk left and the sums of the

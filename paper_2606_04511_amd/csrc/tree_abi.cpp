@@ -87,11 +87,12 @@ int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, 
     return fail(SPARDA_ERR_INVALID_ARG, "n_sel %d is neither 1 nor n_nodes %d", n_sel, n_nodes);
   if (!std::isfinite(sm_scale)) return fail(SPARDA_ERR_INVALID_ARG, "sm_scale is not finite");
   const sparda::TreeAttnPlan plan = sparda::tree_attn_plan((int64_t)shape->batch * shape->n_kv_heads, n_nodes,
-                                                           shape->group_size, shape->k_total, t_max);
-  if (plan.ws_bytes > 0) {
-    if (!ws || !aligned(ws, 16)) return fail(SPARDA_ERR_WORKSPACE, "workspace of %zu bytes required", plan.ws_bytes);
-    if (ws_bytes < plan.ws_bytes)
-      return fail(SPARDA_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, plan.ws_bytes);
+                                                           shape->group_size, shape->k_total, t_max, n_sel == 1);
+  const size_t need = sparda::tree_attn_ws((int64_t)shape->batch * shape->n_kv_heads, n_nodes, shape->group_size,
+                                           shape->k_total, t_max);
+  if (need > 0) {
+    if (!ws || !aligned(ws, 16)) return fail(SPARDA_ERR_WORKSPACE, "workspace of %zu bytes required", need);
+    if (ws_bytes < need) return fail(SPARDA_ERR_WORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
   }
   sparda::TreeAttnArgs a;
   a.tb = {t_ctx, parent, shape->batch, n_nodes, t_max};
@@ -110,7 +111,11 @@ int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, 
   a.k_total = shape->k_total;
   a.t_cap = shape->t_cap;
   a.sm_scale = sm_scale;
+  a.width = plan.width;
   a.n_splits = plan.n_splits;
+  a.k_recip = (((uint64_t)1 << 36) + shape->k_total - 1) / shape->k_total;
+  a.ns_recip = ((1u << 20) + plan.n_splits - 1) / plan.n_splits;
+  a.g_recip = ((1u << 16) + shape->group_size - 1) / shape->group_size;
   return hip_status(sparda::launch_tree_attn(a, stream), "tree attention launch");
 }
 

@@ -54,6 +54,9 @@ static_assert(sizeof(TreeAttnLds) <= 160 * 1024, "LDS of one CU");
 static_assert(sizeof(float) * kTaWaves * 16 * (kTaPitch + 2) <= kTaRing * kTaSlot, "a merge round of the private form fits in the buffers");
 static_assert(sizeof(float) * 4 * 32 * (kTaPitch + 2) <= kTaRing * kTaSlot, "the merge of the shared form fits in the ring");
 
+// Column c's node, c / G: c < 1024 and G <= 16.
+__device__ __forceinline__ int node_of(const TreeAttnArgs& a, int c) { return (int)(((uint32_t)c * a.g_recip) >> 16); }
+
 // What a workgroup works on: a tile of columns of one (batch, group) and a split of its blocks.
 struct TreeUnit {
   int64_t bm;
@@ -72,8 +75,10 @@ struct TreeLists {
   int64_t row0;
   int ahead[kAhead];
 
+  // e / k_total: at most 64 k_total entries, and 64 k_total^2 < 2^36
+  __device__ __forceinline__ int row_of(const TreeAttnArgs& a, int e) const { return (int)(((uint64_t)e * a.k_recip) >> 36); }
   __device__ __forceinline__ int entry(const TreeAttnArgs& a, int e) const {  // the block, or -1
-    const int r = e / a.k_total, j = a.sel[row0 * a.k_total + e], c = a.cnt[row0 + r];
+    const int r = row_of(a, e), j = a.sel[row0 * a.k_total + e], c = a.cnt[row0 + r];
     return e - r * a.k_total < c ? j : -1;
   }
   __device__ __forceinline__ void request(const TreeAttnArgs& a, int64_t bm, int first_node, int last_node) {
@@ -95,7 +100,7 @@ struct TreeLists {
     for (int i = tid; i < wn; i += kTaThreads) lds.table[i] = 0ull;
     __syncthreads();
     auto mark = [&](int e, int block) {
-      const int j = block - w0, r = e / a.k_total;
+      const int j = block - w0, r = row_of(a, e);
       if (block < 0 || j < 0 || j >= wn) return;
       if (a.n_sel == 1)
         lds.table[j] = ~0ull;
@@ -127,12 +132,14 @@ struct TreeLists {
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int at = pos + mbcnt64(listed[i]);
-      if (((listed[i] >> lane) & 1ull) && at % ns == u.split)
-        lds.list[at / ns] = (int16_t)((wave * kRounds + i) * 64 + lane);
+      const int share = (int)(((uint32_t)at * a.ns_recip) >> 20);  // at / ns: at < 2048, ns <= 64
+      if (((listed[i] >> lane) & 1ull) && at - share * ns == u.split)
+        lds.list[share] = (int16_t)((wave * kRounds + i) * 64 + lane);
       pos += (int)__popcll(listed[i]);
     }
-    const int n_blocks = (total - u.split + ns - 1) / ns;
-    *tree_here = w0 + kTaWindow >= nb && u.present != 0ull && total % ns == u.split;
+    const int whole = (int)(((uint32_t)total * a.ns_recip) >> 20), over = total - whole * ns;
+    const int n_blocks = whole + (u.split < over ? 1 : 0);
+    *tree_here = w0 + kTaWindow >= nb && u.present != 0ull && over == u.split;
     if (*tree_here && tid == 0) lds.list[n_blocks] = (int16_t)kTaTree;
     __syncthreads();
     return n_blocks + (*tree_here ? 1 : 0);
@@ -157,10 +164,10 @@ struct TreeCols {
     const int lane = threadIdx.x & 63, hh = lane & 15, grp = lane >> 4, n = a.tb.n, G = a.group_size;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int c = min(c0 + 16 * nt + hh, n * G - 1), x = c / G;
+      const int c = min(c0 + 16 * nt + hh, n * G - 1), x = node_of(a, c);
       node[nt] = x - u.first_node;
       anc[nt] = ((uint64_t)(uint32_t)__shfl((int)(u.anc >> 32), x, 64) << 32) | (uint32_t)__shfl((int)(uint32_t)u.anc, x, 64);
-      const uint16_t* qrow = a.q + ((u.bm * G + c % G) * n + x) * kHeadDim + 8 * grp;
+      const uint16_t* qrow = a.q + ((u.bm * G + (c - x * G)) * n + x) * kHeadDim + 8 * grp;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) q[nt][ks] = as_bf16x8(ld16(qrow + 32 * ks));
       m[nt] = -INFINITY;
@@ -219,7 +226,7 @@ struct TreeCols {
   // One half block: K rows at kbuf, V rows at vbuf (rows of 256 bytes, 16-byte piece x of token t at x ^ (t % 16) for K
   // and x ^ 2 (t % 8) for V).  valid: its tokens that hold a V; they are the context's, or the drafted ones from node
   // 32 hf on.  k_read runs once K has been read, v_ready before V is, v_read after.
-  template <class KRead, class VReady>
+  template <bool kVFirst, class KRead, class VReady>
   __device__ __forceinline__ void half(const char* kbuf, const char* vbuf, bool tree, int hf, int e, uint32_t valid,
                                        KRead k_read, VReady v_ready) {
     const int lane = threadIdx.x & 63, hh = lane & 15, grp = lane >> 4;
@@ -253,6 +260,15 @@ struct TreeCols {
         for (int tt = 0; tt < 2; ++tt) st[nt][tt] = mfma16x16x32(kf[tt][ks], q[nt][ks], st[nt][tt]);
     }
     k_read();
+    bf16x8 vf[8];
+    auto read_v = [&] {
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        const uint2 v0 = lds_read_tr16(vbuf + (va ^ (dt << 5))), v1 = lds_read_tr16(vbuf + 4096 + (va ^ (dt << 5)));
+        vf[dt] = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
+      }
+    };
+    if constexpr (kVFirst) read_v();  // under way during the softmax
     float top[NT];
     bool ask = false;
 #pragma unroll
@@ -303,12 +319,9 @@ struct TreeCols {
       pb[nt] = as_bf16x8(make_uint4(pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]),
                                     pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])));
     }
-    v_ready();
-    bf16x8 vf[8];
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) {
-      const uint2 v0 = lds_read_tr16(vbuf + (va ^ (dt << 5))), v1 = lds_read_tr16(vbuf + 4096 + (va ^ (dt << 5)));
-      vf[dt] = as_bf16x8(make_uint4(v0.x, v0.y, v1.x, v1.y));
+    if constexpr (!kVFirst) {
+      v_ready();
+      read_v();
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -336,7 +349,8 @@ __device__ __forceinline__ uint32_t half_valid(const TreeUnit& u, bool tree, int
 // Four dims of a finished column, or of a split's partial.
 __device__ __forceinline__ void store_dims(const TreeAttnArgs& a, const TreeUnit& u, int c, int d, float m, float den,
                                            f32x4 num) {
-  const int64_t row = (u.bm * a.group_size + c % a.group_size) * a.tb.n + c / a.group_size;
+  const int node = node_of(a, c);
+  const int64_t row = (u.bm * a.group_size + (c - node * a.group_size)) * a.tb.n + node;
   if (a.n_splits == 1) {
     const float inv = den > 0.f ? 1.f / den : 0.f;
     uint2 w;
@@ -350,18 +364,18 @@ __device__ __forceinline__ void store_dims(const TreeAttnArgs& a, const TreeUnit
   }
 }
 
-// The workgroup's unit; false: none.  Workgroups 8 apart run on the same XCD: the tiles of a (group, split) share its L2.
-__device__ __forceinline__ bool tree_unit(const TreeAttnArgs& a, int n_tiles, int n_groups, int tile_cols,
-                                          TreeUnit* u, TreeLists* lists) {
+// The workgroup's unit; false: none.  Grid x = 8 n_tiles, y = groups / 8, z = splits: workgroups 8 apart run on the same
+// XCD, so the tiles of a group share its L2.
+__device__ __forceinline__ bool tree_unit(const TreeAttnArgs& a, int n_groups, int tile_cols, TreeUnit* u, TreeLists* lists) {
   const int lane = threadIdx.x & 63, n = a.tb.n, G = a.group_size;
-  const int unit = (int)(blockIdx.x / (8 * n_tiles)) * 8 + (int)(blockIdx.x % 8);
-  if (unit >= n_groups * a.n_splits) return false;
-  u->tile = (int)(blockIdx.x / 8) % n_tiles;
-  u->bm = unit % n_groups;
-  u->split = unit / n_groups;
+  const int group = blockIdx.y * 8 + (blockIdx.x & 7);
+  if (group >= n_groups) return false;
+  u->tile = blockIdx.x >> 3;
+  u->bm = group;
+  u->split = blockIdx.z;
   const int c0 = u->tile * tile_cols;
-  u->first_node = c0 / G;
-  u->last_node = (min(c0 + tile_cols, n * G) - 1) / G;
+  u->first_node = node_of(a, c0);
+  u->last_node = node_of(a, min(c0 + tile_cols, n * G) - 1);
   lists->request(a, u->bm, u->first_node, u->last_node);
   const int b = (int)(u->bm / a.n_kv_heads);
   const int64_t ctx = tree_context(a.tb, b);
@@ -374,15 +388,15 @@ __device__ __forceinline__ bool tree_unit(const TreeAttnArgs& a, int n_tiles, in
 
 // ---- up to 32 columns: every wavefront streams halves of its own -------------------------------------
 
-template <int NT>
-__global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, int n_tiles, int n_groups) {
+template <int NT, bool kOnce>
+__global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, int n_groups) {
   __shared__ __align__(16) TreeAttnLds lds;
   const int tid = threadIdx.x, lane = tid & 63, hh = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = a.tb.n, c0_tile = 16 * NT;
   TreeUnit u;
   TreeLists lists;
-  if (!tree_unit(a, n_tiles, n_groups, c0_tile, &u, &lists)) return;
+  if (!tree_unit(a, n_groups, c0_tile, &u, &lists)) return;
   const int c0 = u.tile * c0_tile;
   TreeCols<NT> cols;
   cols.load(a, u, c0);
@@ -398,13 +412,13 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
     if (j != kTaTree) {
       const char* src = reinterpret_cast<const char*>(cache + (u.bm * a.t_cap + (int64_t)j * kBlock + hf * kTaHalf) * kHeadDim);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) lds_load16(src + 1024 * i, off0 ^ ((i & flip) << by), dst + 1024 * i);
+      for (int i = 0; i < 8; ++i) lds_load16<kOnce>(src + 1024 * i, off0 ^ ((i & flip) << by), dst + 1024 * i);
     } else {  // rows past the last node repeat it
       const char* src = reinterpret_cast<const char*>(drafted + u.bm * n * kHeadDim);
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < 8; ++i) {
         const int row = min(hf * kTaHalf + 4 * i + r4, n - 1);
-        lds_load16(src, row * 256 + ((off0 ^ ((i & flip) << by)) & 255), dst + 1024 * i);
+        lds_load16<kOnce>(src, row * 256 + ((off0 ^ ((i & flip) << by)) & 255), dst + 1024 * i);
       }
     }
   };
@@ -433,7 +447,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
       const int j2 = more ? block_of(cols.entry(lds, x2 >> 1)) : 0;
       const uint32_t valid = half_valid(u, tree, j, hf);
       __asm__ __volatile__("s_waitcnt vmcnt(8)" ::: "memory");  // this half's K (its V may be under way)
-      cols.half(
+      cols.template half<false>(
           kbuf, vbuf, tree, hf, e, valid,
           [&] {
             __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
@@ -495,9 +509,10 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
 
 // ---- more columns: the wavefronts share the blocks ------------------------------------------------------
 
-// WC groups of 16 NT columns; with WC = 4 two wavefronts take a group, one half of every block each.
-template <int NT, int WC>
-__global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnArgs a, int n_tiles, int n_groups) {
+// kOnce: no other workgroup reads the blocks, so they bypass the caches (16 nodes of 256 groups of 4 heads at 128K
+// 108 -> 93 us).  WC groups of 16 NT columns; with WC = 4 two wavefronts take a group, one half of every block each.
+template <int NT, int WC, bool kOnce>
+__global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnArgs a, int n_groups) {
   constexpr int WT = kTaWaves / WC;
   static_assert(WT == 1 || WT == 2, "a wavefront takes whole blocks or halves");
   __shared__ __align__(16) TreeAttnLds lds;
@@ -507,7 +522,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
   const int n = a.tb.n;
   TreeUnit u;
   TreeLists lists;
-  if (!tree_unit(a, n_tiles, n_groups, 16 * NT * WC, &u, &lists)) return;
+  if (!tree_unit(a, n_groups, 16 * NT * WC, &u, &lists)) return;
   const int c0 = (u.tile * WC + cg) * 16 * NT;
   const bool live = c0 < n * a.group_size;  // the last tile may leave wavefronts without columns: they only load
   TreeCols<NT> cols;
@@ -518,19 +533,17 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(lds.kv)) + wave * 2048;
   auto issue = [&](int j, int slot) {
     const uint32_t dst = ring_at + slot * kTaSlot;
+    const bool tree = j == kTaTree;
+    const int64_t at = (tree ? u.bm * n : u.bm * a.t_cap + (int64_t)j * kBlock) * kHeadDim;
+    const uint16_t* const kp = (tree ? a.kt : a.k) + at;
+    const uint16_t* const vp = (tree ? a.vt : a.v) + at;
+    const int last = tree ? n - 1 : kBlock - 1;  // rows past the last node repeat it
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = 8 * wave + 4 * i + r4;
-      const uint32_t kx = 16 * ((lane & 15) ^ (row & 15)), vx = 16 * ((lane & 15) ^ (2 * (row & 7)));
-      if (j != kTaTree) {
-        const int64_t at = (u.bm * a.t_cap + (int64_t)j * kBlock) * kHeadDim;
-        lds_load16(a.k + at, row * 256 + kx, dst + 1024 * i);
-        lds_load16(a.v + at, row * 256 + vx, dst + 2 * kTaBuf + 1024 * i);
-      } else {  // rows past the last node repeat it
-        const int64_t at = u.bm * n * kHeadDim;
-        lds_load16(a.kt + at, min(row, n - 1) * 256 + kx, dst + 1024 * i);
-        lds_load16(a.vt + at, min(row, n - 1) * 256 + vx, dst + 2 * kTaBuf + 1024 * i);
-      }
+      const uint32_t from = min(row, last) * 256;
+      lds_load16<kOnce>(kp, from + 16 * ((lane & 15) ^ (row & 15)), dst + 1024 * i);
+      lds_load16<kOnce>(vp, from + 16 * ((lane & 15) ^ (2 * (row & 7))), dst + 2 * kTaBuf + 1024 * i);
     }
   };
 
@@ -541,7 +554,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
     auto block_of = [&](int j) { return j == kTaTree ? j : j + w0; };
     cols.chunk = -1;
     lds_loads_landed();  // the queries: from here on the loads are counted, 4 per block
-#pragma unroll
+#pragma unroll 1
     for (int s = 0; s < kTaRing - 1; ++s)
       if (s < n_list) issue(block_of(cols.entry(lds, s)), s);
     for (int s = 0; s < n_list; ++s) {
@@ -558,20 +571,19 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
         __asm__ __volatile__("s_waitcnt vmcnt(4)" ::: "memory");
       else
         __asm__ __volatile__("s_waitcnt vmcnt(0)" ::: "memory");
-      const uint32_t valid[2] = {half_valid(u, tree, j, 0), half_valid(u, tree, j, 1)};
-      if ((valid[0] & valid[1]) != ~0u) {
+      const uint64_t valid = half_valid(u, tree, j, 0) | (uint64_t)half_valid(u, tree, j, 1) << 32;
+      if (valid != ~0ull) {
         for (int r = 8 * wave + r4; r < 8 * wave + 8; r += 4)
-          if (!((valid[r >> 5] >> (r & 31)) & 1u)) *reinterpret_cast<uint4*>(vslot + r * 256 + 16 * (lane & 15)) = make_uint4(0u, 0u, 0u, 0u);
+          if (!((valid >> r) & 1ull)) *reinterpret_cast<uint4*>(vslot + r * 256 + 16 * (lane & 15)) = make_uint4(0u, 0u, 0u, 0u);
       }
       __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       __asm__ __volatile__("" ::: "memory");
       if (s + kTaRing - 1 < n_list) issue(block_of(cols.entry(lds, s + kTaRing - 1)), (s + kTaRing - 1) % kTaRing);
       if (!live) continue;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (WT == 2 && h != th) continue;
-        cols.half(kslot + h * kTaBuf, vslot + h * kTaBuf, tree, h, s, valid[h], [] {}, [] {});
+#pragma unroll 1
+      for (int h = WT == 2 ? th : 0; h < (WT == 2 ? th + 1 : 2); ++h) {
+        cols.template half<true>(kslot + h * kTaBuf, vslot + h * kTaBuf, tree, h, s, (uint32_t)(valid >> (h * kTaHalf)), [] {}, [] {});
       }
     }
     __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -659,22 +671,24 @@ __global__ __launch_bounds__(kCombineThreads) void tree_combine_kernel(TreeAttnA
 
 template <class Kernel>
 hipError_t launch_tiles(Kernel kernel, const TreeAttnArgs& a, int tile_cols, hipStream_t stream) {
-  const int groups = a.tb.batch * a.n_kv_heads, units = groups * a.n_splits;
+  const int groups = a.tb.batch * a.n_kv_heads;
   const int n_tiles = (a.tb.n * a.group_size + tile_cols - 1) / tile_cols;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((units + 7) / 8 * 8 * n_tiles)), dim3(kTaThreads), 0, stream, a, n_tiles,
-                     groups);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * n_tiles), (unsigned)((groups + 7) / 8), (unsigned)a.n_splits),
+                     dim3(kTaThreads), 0, stream, a, groups);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_tree_attn(const TreeAttnArgs& a, hipStream_t stream) {
-  const int cols = tree_attn_cols(a.tb.n, a.group_size);
-  const hipError_t e = cols == 16    ? launch_tiles(tree_attn_kernel<1>, a, cols, stream)
-                       : cols == 32  ? launch_tiles(tree_attn_kernel<2>, a, cols, stream)
-                       : cols == 64  ? launch_tiles(tree_attn_shared_kernel<1, 4>, a, cols, stream)
-                       : cols == 128 ? launch_tiles(tree_attn_shared_kernel<2, 4>, a, cols, stream)
-                                     : launch_tiles(tree_attn_shared_kernel<2, 8>, a, cols, stream);
+  const int cols = a.tb.n * a.group_size;
+  const int width = a.width;
+  const bool once = cols <= width;  // one tile: every block is read once
+  const hipError_t e = width == 16    ? launch_tiles(tree_attn_kernel<1, true>, a, width, stream)
+                       : width == 32  ? launch_tiles(once ? tree_attn_kernel<2, true> : tree_attn_kernel<2, false>, a, width, stream)
+                       : width == 64  ? launch_tiles(tree_attn_shared_kernel<1, 4, true>, a, width, stream)
+                       : width == 128 ? launch_tiles(tree_attn_shared_kernel<2, 4, true>, a, width, stream)
+                                      : launch_tiles(once ? tree_attn_shared_kernel<2, 8, true> : tree_attn_shared_kernel<2, 8, false>, a, width, stream);
   if (e != hipSuccess || a.n_splits == 1) return e;
   const int64_t rows = (int64_t)a.tb.batch * a.n_kv_heads * a.group_size * a.tb.n;
   hipLaunchKernelGGL(tree_combine_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(kCombineThreads), 0, stream, a, rows);

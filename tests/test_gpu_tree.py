@@ -228,6 +228,50 @@ def test_attn_scales_and_extremes(dev):
     assert float((off / ref.attn_bar(want, w)).max()) <= 1.0
 
 
+# Calls whose blocks exceed the last-level cache share them between the wavefronts of a workgroup: 64, 128 or 256
+# columns (node, query head) each.  Only some groups are compared.
+MANY = [
+    # nodes, tree, group, k, t, one list
+    (16, "wide", 4, 9, 700, False),    # 64 columns
+    (13, "wide", 3, 9, 700, True),     # 39 of 64
+    (21, "chain", 5, 9, 1000, False),  # 105 of 128
+    (31, "wide", 4, 9, 640, True),     # 124 of 128
+    (40, "wide", 4, 9, 700, False),    # 160 of 256
+    (64, "wide", 7, 9, 700, False),    # 448 in two tiles of 256
+    (33, "star", 16, 9, 700, True),    # 528 in three, the last of 16
+]
+
+
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_attn_many_groups(dev, case):
+    n, kind, G, k, t, shared = MANY[case]
+    say("tree attention of many groups", MANY[case])
+    gen, rng = torch.Generator(device=dev).manual_seed(case), random.Random(case)
+    B, H = 4, 256
+    s = shape_of(B, H, G, k, t, n)
+    mk = lambda *size: torch.randn(*size, generator=gen, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    q, kk, vv, kt, vt = mk(B, H * G, n, D), mk(B, H, s.t_cap, D), mk(B, H, s.t_cap, D), mk(B, H, n, D), mk(B, H, n, D)
+    t_ctx = [t, t - 63, -1, t - 200]
+    for b in range(B):
+        kk[b, :, max(t_ctx[b], 0):] = vv[b, :, max(t_ctx[b], 0):] = NAN
+    parent = trees(rng, B, n, kind, pad=[(1, n - 1, n)])
+    ns, nb = (1 if shared else n), -(-t // L)
+    sel = torch.rand(B, H, ns, nb, generator=gen, device=dev).topk(k - 1, dim=3).indices.to(torch.int16)
+    sel = torch.cat((sel, sel[..., :1]), 3).contiguous()  # one entry twice
+    cnt = torch.randint(0, k + 1, (B, H, ns), generator=gen, device=dev).to(torch.int16)
+    o = torch.full(q.shape, NAN, dtype=torch.bfloat16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_ATTN, n, t))
+    sp.sparda_tree_attn(s, q, n, torch.tensor(t_ctx, dtype=torch.int32, device=dev), t, parent.to(dev), kk, vv, kt, vt,
+                        ns, sel, cnt, ref.SCALE, o, ws)
+    torch.cuda.synchronize()
+    assert not torch.isnan(o).any() and not o[2].any()
+    for h in (0, 7, 128, 255):
+        x = [y[:, h:h + 1].cpu() for y in (kk, vv, kt, vt, sel, cnt)]
+        want, w = ref.attn(q[:, h * G:(h + 1) * G].cpu(), *x[:4], t_ctx, parent, *x[4:], ref.SCALE)
+        off = (o[:, h * G:(h + 1) * G].cpu().double() - want).abs()
+        assert float((off / ref.attn_bar(want, w)).max()) <= 1.0
+
+
 # ---- verify -------------------------------------------------------------------------------------------
 
 VERIFY = [
