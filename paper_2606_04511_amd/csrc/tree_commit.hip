@@ -4,8 +4,12 @@
 //
 // One workgroup per (layer, batch, group).  Its rows are 256 bytes: 16 lanes move a row of K and the
 // same row of V.  A completed window's keys come from the cache up to the context and from the
-// drafted rows behind it, so nothing waits for the copies; float64 sums of at most 64 bf16 keys are
-// exact, so the mean has the bits of sparda_compress_keys.
+// drafted rows behind it, so nothing waits for the copies, and the keys of up to two windows are requested
+// together with the rows; float64 sums of at most 64 bf16 keys are exact, so the mean has the bits of
+// sparda_compress_keys.
+//
+// What bounds it: latency (a dependent chain of the path's loads, the rows and the stores) for few groups, the
+// memory's rate for scattered rows of 256 bytes for many.
 #include "device_util.hpp"
 #include "launch.hpp"
 #include "tree.hpp"
@@ -14,7 +18,9 @@ namespace sparda {
 
 namespace {
 
+template <int L>  // tokens of a window
 __global__ __launch_bounds__(256) void tree_commit_kernel(TreeCommitArgs a) {
+  __shared__ double part[16][144];
   const int tid = threadIdx.x, lane = tid & 63;
   const int groups = a.batch * a.n_kv_heads;
   const int layer = blockIdx.x / groups;
@@ -34,6 +40,23 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(TreeCommitArgs a) {
   const uint4* vt = reinterpret_cast<const uint4*>(a.vt[layer] + bm * a.n * kHeadDim);
   uint4* k = reinterpret_cast<uint4*>(a.k[layer] + bm * a.t_cap * kHeadDim);
   uint4* v = reinterpret_cast<uint4*>(a.v[layer] + bm * a.t_cap * kHeadDim);
+  if (cnt == 0) return;
+  // ---- windows [w0, w1) that the tokens complete
+  const int64_t w0 = a.kc[layer] ? grid_win_vis(a.grid, t - 1) + 1 : 0;
+  int64_t w1 = a.kc[layer] ? grid_win_vis(a.grid, t + cnt - 1) + 1 : 0;
+  if (w1 > a.nc_cap) w1 = a.nc_cap;
+  // row rr of window w: in the cache, or drafted (the path's nodes are in the lanes of every wavefront)
+  auto key_row = [&](int64_t w, int rr) {
+    const int64_t tok = w * a.grid.s + rr;
+    const int node = __shfl(mine, (int)(tok < t ? 0 : tok - t) & 63, 64);
+    return tok < t ? k[tok * kPieces + c] : kt[node * kPieces + c];
+  };
+  constexpr int kRows = L / 16;  // of a window that a thread sums
+  uint4 first[kRows];
+  if (w0 < w1) {
+#pragma unroll
+    for (int x = 0; x < kRows; ++x) first[x] = key_row(w0, r + 16 * x);
+  }
   for (int i0 = 0; i0 < cnt; i0 += 16) {
     const int i = i0 + r;
     const int node = __shfl(mine, i & 63, 64);
@@ -43,21 +66,31 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(TreeCommitArgs a) {
       v[(t + i) * kPieces + c] = y;
     }
   }
-  if (a.kc[layer] == nullptr || cnt == 0) return;
-  const int64_t w0 = grid_win_vis(a.grid, t - 1) + 1;
-  int64_t w1 = grid_win_vis(a.grid, t + cnt - 1) + 1;
-  if (w1 > a.nc_cap) w1 = a.nc_cap;
-  const uint16_t* keys = a.k[layer] + bm * a.t_cap * kHeadDim;
-  const uint16_t* drafted = a.kt[layer] + bm * a.n * kHeadDim;
-  for (int64_t w = w0 + (tid >> 7); w < w1; w += 2) {
-    double sum = 0.0;
-    for (int x = 0; x < a.grid.l; ++x) {
-      const int64_t tok = w * a.grid.s + x;
-      const uint16_t* row = tok < t ? keys + tok * kHeadDim
-                                    : drafted + (int64_t)a.path[(int64_t)b * a.n + (tok - t)] * kHeadDim;
-      sum += (double)bf16_to_f32(row[tid & 127]);
+  // ---- the windows' means: dims 8 c + e at 9 c + e of a thread's row of partial sums (no bank conflicts)
+  for (int64_t w = w0; w < w1; ++w) {
+    double acc[8] = {};
+#pragma unroll
+    for (int x = 0; x < kRows; ++x) {
+      const uint4 y = first[x];
+      acc[0] += bf16lo(y.x); acc[1] += bf16hi(y.x);
+      acc[2] += bf16lo(y.y); acc[3] += bf16hi(y.y);
+      acc[4] += bf16lo(y.z); acc[5] += bf16hi(y.z);
+      acc[6] += bf16lo(y.w); acc[7] += bf16hi(y.w);
     }
-    a.kc[layer][(bm * a.nc_cap + w) * kHeadDim + (tid & 127)] = f64_to_bf16(sum / a.grid.l);
+    if (w + 1 < w1) {
+#pragma unroll
+      for (int x = 0; x < kRows; ++x) first[x] = key_row(w + 1, r + 16 * x);
+    }
+    __syncthreads();  // the last window's sums have been read
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[r][c * 9 + e] = acc[e];
+    __syncthreads();
+    if (tid < kHeadDim) {
+      double sum = 0.0;
+#pragma unroll
+      for (int g = 0; g < 16; ++g) sum += part[g][(tid >> 3) * 9 + (tid & 7)];
+      a.kc[layer][(bm * a.nc_cap + w) * kHeadDim + tid] = f64_to_bf16(sum * (1.0 / L));  // exact: L is a power of 2
+    }
   }
 }
 
@@ -65,7 +98,10 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(TreeCommitArgs a) {
 
 hipError_t launch_tree_commit(const TreeCommitArgs& a, hipStream_t stream) {
   const int64_t wgs = (int64_t)a.n_layers * a.batch * a.n_kv_heads;
-  hipLaunchKernelGGL(tree_commit_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  if (a.grid.l == 64)
+    hipLaunchKernelGGL(tree_commit_kernel<64>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(tree_commit_kernel<32>, dim3((unsigned)wgs), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
