@@ -27,13 +27,20 @@ __device__ __forceinline__ SeqGeom seq_geom(const TreeBatch& tb, int b, int lane
 
 // Block scores of all nodes of a (batch, group) on MFMA: the keys are read once.  A = 16 nodes' Forecast
 // rows (MT of them in registers), B = 16 keys, so consecutive candidates lie in consecutive lanes.  A step
-// is 64 keys, all requested before the first product: 64 blocks on the one-key-per-block grid, 16 blocks
-// of the (32, 16) grid as four tiles, tile u holding window u of each block.  Window -1 of a block is
-// window 3 of the one before: the neighbouring lane's score, or for lane 0 that of the last step (at a
-// wavefront's first step one more key).
+// is 64 consecutive keys, which go from memory into 16 KiB of the wavefront's own LDS in whole rows (read as
+// fragments of 64 bytes per row straight from memory the same launch is 7 us longer) and from there into
+// registers, so that the next step's are under way during the products: 64 blocks on the one-key-per-block grid, 16
+// blocks of the (32, 16) grid as four tiles, tile u holding window u of each block.  Window -1 of a block is window 3
+// of the one before: the neighbouring lane's score, or for lane 0 that of the last step (at a wavefront's first step one
+// more key).
+//
+// What bounds it: the memory's rate and what frames it.  16 nodes of 256 groups at 128K (134 MB of keys, 33 MB of
+// scores): 29 us; the top-k of their 4096 rows another 25, its own chain of counts and the one load (see
+// row_topk_kernel).
 template <bool kBlocks, int MT>
 __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n_groups, int steps) {
   constexpr int kPerStep = kBlocks ? 64 : 16;  // candidates
+  __shared__ __align__(16) char bufs[4][64 * 256];
   const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t bm = blockIdx.x % n_groups;
@@ -84,14 +91,29 @@ __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n
       if (w < 0 || w > vis) carry[mt] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     }
   }
+  // a step's 64 keys, 4 per instruction; piece y of key row z lies at y ^ c, c the lane column that reads the row
+  const int r4 = lane >> 4;
+  const uint32_t buf_at = __builtin_amdgcn_readfirstlane(lds_address(bufs[wave]));
+  const uint16_t* const rows = a.kc + bm * a.nc_cap * kHeadDim;
+  auto request = [&](int x) {
+    const int w0 = kBlocks ? g.cand_lo + x : 4 * (g.cand_lo + x);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int z = 4 * i + r4, col = kBlocks ? z & 15 : i;
+      lds_load16<true>(rows, (uint32_t)max(min(w0 + z, vis), 0) * 256 + 16 * ((lane & 15) ^ col), buf_at + 1024 * i);
+    }
+  };
+  request(x0);
   for (; x0 < x_end; x0 += kPerStep) {
+    lds_loads_landed();
     uint4 kw[4][4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const uint16_t* src = key_at(kBlocks ? g.cand_lo + x0 + 16 * u + c : 4 * (g.cand_lo + x0 + c) + u);
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) kw[u][ks] = ld16_nt(src + 32 * ks);
-    }
+      for (int ks = 0; ks < 4; ++ks)
+        kw[u][ks] = *reinterpret_cast<const uint4*>(&bufs[wave][(kBlocks ? 16 * u + c : 4 * c + u) * 256 + 16 * ((4 * ks + q) ^ c)]);
+    __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory");  // the keys are in registers
+    if (x0 + kPerStep < x_end) request(x0 + kPerStep);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if constexpr (kBlocks) {
@@ -122,9 +144,9 @@ template <bool kBlocks>
 hipError_t launch_scores(const TreeSelectArgs& a, int C, hipStream_t stream) {
   const int groups = a.tb.batch * a.n_kv_heads;
   const int total = (C + (kBlocks ? 64 : 16) - 1) / (kBlocks ? 64 : 16);
-  // steps per wavefront: one while the chip is not full, at most 8
+  // steps per wavefront: one while the chip is not full, else about two wavefronts per SIMD; at most 16
   const int64_t all = (int64_t)groups * total;
-  const int steps = (int)(all <= 8192 ? 1 : all >= 65536 ? 8 : all / 8192);
+  const int steps = (int)(all <= 2048 ? 1 : all >= 16 * 2048 ? 16 : all / 2048);
   const int parts = (total + steps - 1) / steps;
   const dim3 grid((unsigned)(groups * ((parts + 3) / 4))), block(256);
   switch ((a.tb.n + 15) / 16) {
