@@ -231,7 +231,7 @@ def test_attn_scales_and_extremes(dev):
 # Calls whose blocks exceed the last-level cache share them between the wavefronts of a workgroup: 64, 128 or 256
 # columns (node, query head) each.  Only some groups are compared.
 MANY = [
-    # nodes, tree, group, k, t, one list
+    # nodes, tree, group, k, t, one list; 1024 groups, or as many as said
     (16, "wide", 4, 9, 700, False),    # 64 columns
     (13, "wide", 3, 9, 700, True),     # 39 of 64
     (21, "chain", 5, 9, 1000, False),  # 105 of 128
@@ -239,22 +239,22 @@ MANY = [
     (40, "wide", 4, 9, 700, False),    # 160 of 256
     (64, "wide", 7, 9, 700, False),    # 448 in two tiles of 256
     (33, "star", 16, 9, 700, True),    # 528 in three, the last of 16
+    (16, "wide", 4, 260, 140000, True, 1, 32),  # more than 2048 blocks
 ]
 
 
 @pytest.mark.parametrize("case", range(len(MANY)))
 def test_attn_many_groups(dev, case):
-    n, kind, G, k, t, shared = MANY[case]
+    n, kind, G, k, t, shared, B, H = (MANY[case] + (4, 256))[:8]
     say("tree attention of many groups", MANY[case])
     gen, rng = torch.Generator(device=dev).manual_seed(case), random.Random(case)
-    B, H = 4, 256
     s = shape_of(B, H, G, k, t, n)
     mk = lambda *size: torch.randn(*size, generator=gen, device=dev, dtype=torch.bfloat16)  # noqa: E731
     q, kk, vv, kt, vt = mk(B, H * G, n, D), mk(B, H, s.t_cap, D), mk(B, H, s.t_cap, D), mk(B, H, n, D), mk(B, H, n, D)
-    t_ctx = [t, t - 63, -1, t - 200]
+    t_ctx = [t, t - 63, -1, t - 200][:B]
     for b in range(B):
         kk[b, :, max(t_ctx[b], 0):] = vv[b, :, max(t_ctx[b], 0):] = NAN
-    parent = trees(rng, B, n, kind, pad=[(1, n - 1, n)])
+    parent = trees(rng, B, n, kind, pad=[(B - 1, n - 1, n)])
     ns, nb = (1 if shared else n), -(-t // L)
     sel = torch.rand(B, H, ns, nb, generator=gen, device=dev).topk(k - 1, dim=3).indices.to(torch.int16)
     sel = torch.cat((sel, sel[..., :1]), 3).contiguous()  # one entry twice
@@ -264,8 +264,8 @@ def test_attn_many_groups(dev, case):
     sp.sparda_tree_attn(s, q, n, torch.tensor(t_ctx, dtype=torch.int32, device=dev), t, parent.to(dev), kk, vv, kt, vt,
                         ns, sel, cnt, ref.SCALE, o, ws)
     torch.cuda.synchronize()
-    assert not torch.isnan(o).any() and not o[2].any()
-    for h in (0, 7, 128, 255):
+    assert not torch.isnan(o).any() and not o[2:3].any()
+    for h in (0, 7, H // 2, H - 1):
         x = [y[:, h:h + 1].cpu() for y in (kk, vv, kt, vt, sel, cnt)]
         want, w = ref.attn(q[:, h * G:(h + 1) * G].cpu(), *x[:4], t_ctx, parent, *x[4:], ref.SCALE)
         off = (o[:, h * G:(h + 1) * G].cpu().double() - want).abs()
@@ -546,3 +546,67 @@ def test_steps_together_follow_ordinary_decode(dev, grid):
             assert torch.equal(kc0[b, :, :w].view(torch.int16), kc1[b, :, :w].view(torch.int16))
     say(f"  {total} tokens in 8 steps of {B} sequences, lengths {t.tolist()}")
     assert total > 8 * B
+
+
+def test_captured_step_replays(dev):
+    """One step captured into a graph on a side stream and replayed with other lengths, trees and probabilities, with
+    eager steps on the same buffers' copies in between: every replay gives the eager results."""
+    B, H, G, n, k, V, t_cap = 2, 2, 4, 11, 6, 3000, 2048
+    s = shape_of(B, H, G, k, 0, n, t_cap=t_cap)
+    t_max, rng = 1500, random.Random(1)
+    gen = torch.Generator(device=dev).manual_seed(1)
+    mk = lambda *size: torch.randn(*size, generator=gen, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    x = {"f": mk(B, H, n, D), "q": mk(B, H * G, n, D), "kt": mk(B, H, n, D), "vt": mk(B, H, n, D),
+         "k": mk(B, H, t_cap, D), "v": mk(B, H, t_cap, D), "kc": mk(B, H, s.nc_cap, D),
+         "t": torch.zeros(B, dtype=torch.int32, device=dev), "parent": trees(rng, B, n, "wide").to(dev),
+         "p": torch.softmax(torch.randn(B, n, V, generator=gen, device=dev), 2),
+         "pq": torch.softmax(torch.randn(B, n, V, generator=gen, device=dev), 2),
+         "tok": torch.zeros(B, n, dtype=torch.int32, device=dev), "u": torch.rand(B, n, generator=gen, device=dev)}
+
+    def outputs():
+        i32 = dict(dtype=torch.int32, device=dev)
+        return {"sel": torch.empty(B, H, n, k, dtype=torch.int16, device=dev), "o": torch.empty_like(x["q"]),
+                "cnt": torch.empty(B, H, n, dtype=torch.int16, device=dev), "path": torch.empty(B, n, **i32),
+                "n_path": torch.empty(B, **i32), "next": torch.empty(B, **i32), "t_new": torch.empty(B, **i32),
+                "ws": [workspace(dev, b) for b in (sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_SELECT, n, t_max),
+                                                   sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_ATTN, n, t_max),
+                                                   sp.sparda_tree_verify_workspace_size(s, n, V))]}
+
+    def step(x, y):
+        sp.sparda_tree_select(s, x["f"], n, x["t"], t_max, x["parent"], x["kc"], y["sel"], y["cnt"], y["ws"][0])
+        sp.sparda_tree_attn(s, x["q"], n, x["t"], t_max, x["parent"], x["k"], x["v"], x["kt"], x["vt"], n, y["sel"],
+                            y["cnt"], ref.SCALE, y["o"], y["ws"][1])
+        sp.sparda_tree_verify(s, n, V, V, sp.SPARDA_PROB_F32, x["p"], x["pq"], x["tok"], x["parent"], x["u"], y["path"],
+                              y["n_path"], y["next"], y["ws"][2])
+        sp.sparda_tree_commit(s, n, x["t"], y["path"], y["n_path"], 1, [x["kt"]], [x["vt"]], [x["k"]], [x["v"]],
+                              [x["kc"]], y["t_new"])
+
+    def vary(i):
+        x["t"].copy_(torch.tensor([1500 - 37 * i, 3 + 300 * i], dtype=torch.int32))
+        x["parent"].copy_(trees(rng, B, n, "chain" if i == 2 else "wide"))
+        x["p"].copy_(torch.softmax(torch.randn(B, n, V, generator=gen, device=dev) * 2, 2))
+        x["tok"].copy_(torch.randint(0, V, (B, n), generator=gen, device=dev))
+        x["u"].copy_(torch.rand(B, n, generator=gen, device=dev) * 0.3)
+
+    side = torch.cuda.Stream()
+    y = outputs()
+    vary(0)
+    with torch.cuda.stream(side):
+        step(x, y)
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step(x, y)
+    for i in range(5):
+        vary(i)
+        torch.cuda.synchronize()
+        alone, out = {a: b.clone() for a, b in x.items()}, outputs()
+        g.replay()
+        torch.cuda.synchronize()
+        step(alone, out)
+        torch.cuda.synchronize()
+        for a in ("sel", "cnt", "o", "path", "n_path", "next", "t_new"):
+            assert torch.equal(y[a], out[a]), (i, a)
+        for a in ("k", "v", "kc"):
+            assert torch.equal(x[a].view(torch.int16), alone[a].view(torch.int16)), (i, a)
+        y["o"].fill_(NAN)
