@@ -52,7 +52,8 @@ struct TreeAttnArgs {
   int64_t t_cap;
   float sm_scale;
   int32_t width, n_splits;  // the plan
-  uint64_t k_recip;    // ceil(2^36 / k_total)
+  uint64_t k_recip;       // ceil(2^36 / k_total)
+  uint64_t groups_recip;  // ceil(2^36 / (batch * n_kv_heads))
   uint32_t ns_recip;   // ceil(2^20 / n_splits)
   uint32_t g_recip;    // ceil(2^16 / group_size)
 };

@@ -114,6 +114,8 @@ int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, 
   a.width = plan.width;
   a.n_splits = plan.n_splits;
   a.k_recip = (((uint64_t)1 << 36) + shape->k_total - 1) / shape->k_total;
+  a.groups_recip = (((uint64_t)1 << 36) + (uint64_t)shape->batch * shape->n_kv_heads - 1) /
+                   ((uint64_t)shape->batch * shape->n_kv_heads);
   a.ns_recip = ((1u << 20) + plan.n_splits - 1) / plan.n_splits;
   a.g_recip = ((1u << 16) + shape->group_size - 1) / shape->group_size;
   return hip_status(sparda::launch_tree_attn(a, stream), "tree attention launch");

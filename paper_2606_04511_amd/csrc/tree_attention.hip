@@ -364,15 +364,15 @@ __device__ __forceinline__ void store_dims(const TreeAttnArgs& a, const TreeUnit
   }
 }
 
-// The workgroup's unit; false: none.  Grid x = 8 n_tiles, y = groups / 8, z = splits: workgroups 8 apart run on the same
-// XCD, so the tiles of a group share its L2.
+// The workgroup's unit; false: none.  Grid x = 8 n_tiles, y = (groups x splits) / 8: workgroups 8 apart run on the same
+// XCD, so the tiles of a (group, split) share its L2, and few groups still spread over all XCDs.
 __device__ __forceinline__ bool tree_unit(const TreeAttnArgs& a, int n_groups, int tile_cols, TreeUnit* u, TreeLists* lists) {
   const int lane = threadIdx.x & 63, n = a.tb.n, G = a.group_size;
-  const int group = blockIdx.y * 8 + (blockIdx.x & 7);
-  if (group >= n_groups) return false;
+  const int unit = blockIdx.y * 8 + (blockIdx.x & 7);
+  if (unit >= n_groups * a.n_splits) return false;
   u->tile = blockIdx.x >> 3;
-  u->bm = group;
-  u->split = blockIdx.z;
+  u->split = a.n_splits == 1 ? 0 : (int)(((uint64_t)unit * a.groups_recip) >> 36);  // with splits: below 2^14 units
+  u->bm = unit - u->split * n_groups;
   const int c0 = u->tile * tile_cols;
   u->first_node = node_of(a, c0);
   u->last_node = node_of(a, min(c0 + tile_cols, n * G) - 1);
@@ -673,8 +673,8 @@ template <class Kernel>
 hipError_t launch_tiles(Kernel kernel, const TreeAttnArgs& a, int tile_cols, hipStream_t stream) {
   const int groups = a.tb.batch * a.n_kv_heads;
   const int n_tiles = (a.tb.n * a.group_size + tile_cols - 1) / tile_cols;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * n_tiles), (unsigned)((groups + 7) / 8), (unsigned)a.n_splits),
-                     dim3(kTaThreads), 0, stream, a, groups);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * n_tiles), (unsigned)((groups * a.n_splits + 7) / 8)), dim3(kTaThreads), 0,
+                     stream, a, groups);
   return hipGetLastError();
 }
 
