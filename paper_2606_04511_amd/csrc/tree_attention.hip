@@ -2,17 +2,19 @@
 // and their ancestors (paper Sec. 4.1, Eq. 5 over the set of Eq. 1):
 //   o_i = softmax(sm_scale q_i K^T) V over {t' < t in the blocks of node i} U A(i).
 //
-// Work unit: a tile of up to 16 NT columns (column c is query head c % G of node c / G) of one (batch,
-// group), and a split of the blocks that any of the tile's nodes lists.  One pass over K and V serves all
-// columns of the tile, with the running maximum and sum of the softmax in registers.
+// Work unit: a tile of columns (column c is query head c % G of node c / G) of one (batch, group), and a
+// split of the blocks that any of the tile's nodes lists, on one workgroup of 8 wavefronts.  One pass over
+// K and V serves all columns of the tile, with the running maximum and sum of the softmax in registers.
 //   1. The lists of the tile's nodes become a table in LDS, one 64-bit mask of nodes per block (entries
 //      outside the context are dropped, a repeated one sets its bit again), and the blocks with a mask
 //      an ascending list.  Split s takes every n_splits-th of them.  The drafted tokens are one more
 //      entry.  Contexts of more than 2048 blocks are walked in windows of 2048.
-//   2. Each of the 8 wavefronts takes halves of blocks (32 tokens, 8 KiB of K and of V) in turn.  They go
-//      from memory straight into two LDS buffers of its own, the next half's K in flight from the moment
-//      the products of this one have read K, its V from the moment O has read V; the wavefront waits for
-//      its own loads by count, and no barrier joins the wavefronts until the merge.
+//   2. K and V go from memory straight into LDS.  Up to 32 columns (tree_attn_kernel) each wavefront takes
+//      halves of blocks (32 tokens, 8 KiB of K and of V) in turn into two buffers of its own, the next
+//      half's K in flight from the moment the products of this one have read K, its V from the moment O
+//      has read V; it waits for its own loads by count, and no barrier joins the wavefronts until the
+//      merge.  64 to 256 columns (tree_attn_shared_kernel): a ring of four blocks for all wavefronts, each
+//      of which has 16 or 32 columns; one barrier per block.  tree_attn_plan chooses, with figures.
 //   3. Per half and 16 columns: S^T = K Q^T on v_mfma_f32_16x16x32_bf16 (lane (c, g) holds column c's
 //      scores of tokens 16 tt + 4 g + i); masks; P = 2^(z - m) with a reference m that moves only when a
 //      score exceeds it by more than 2^8; O^T += V^T P^T on the same MFMA, V read through the transposing
@@ -20,6 +22,13 @@
 //      weight is off by at most 2^-8 of itself).
 //   4. The wavefronts' states merge through LDS; with splits their float32 partials go to the workspace
 //      and a second launch merges them.
+//
+// What bounds it.  16 nodes of 256 groups of 4 heads at 128K, 64 blocks (537 MB): 91 us, 5.9 TB/s, the memory's rate
+// with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 93 us, of which 9 before the
+// first product, 3 after the last; each of the 48 blocks of a workgroup takes 1.7 us, three blocks' loads in flight.
+// 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 100-116 us, a block read from L2 once per two nodes
+// (256 columns per workgroup: 143, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 13
+// us and 4 for the merge of the splits, a chain of latencies.
 #include <math.h>
 
 #include "device_util.hpp"
