@@ -35,8 +35,7 @@ __device__ __forceinline__ SeqGeom seq_geom(const TreeBatch& tb, int b, int lane
 // more key).
 //
 // What bounds it: the memory's rate and what frames it.  16 nodes of 256 groups at 128K (134 MB of keys, 33 MB of
-// scores): 29 us; the top-k of their 4096 rows another 25, its own chain of counts and the one load (see
-// row_topk_kernel).
+// scores): 29 us; the top-k of their 4096 rows another 17.
 template <bool kBlocks, int MT>
 __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n_groups, int steps) {
   constexpr int kPerStep = kBlocks ? 64 : 16;  // candidates
@@ -158,11 +157,94 @@ hipError_t launch_scores(const TreeSelectArgs& a, int C, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// One wavefront's exact top-k over C <= 64 R scores in its registers (candidate 64 i + lane is x[i]; 0 < n < C; ties to
+// the lower index), by value bins: 256 equal-width bins over the scores' range (a higher bin holds only larger scores),
+// a histogram in LDS, the bin that holds the n-th largest by a scan from the top, that bin's scores ranked one per lane.
+// Returns false, with nothing written, where the bins cannot rank: a range that is empty or not finite, a NaN (also past
+// C: x repeats the last score there), or more than 64 scores in that bin.  lds: 256 uint32.  Against the counting search (reg_topk_emit), whose every threshold
+// costs a count over all the scores: 4096 rows of 2045 candidates 17.4 us and 25, 1344 rows of 508 6.6 and 12.
+template <int R>
+__device__ __forceinline__ bool bin_topk_emit(const float (&x)[R], int C, int n, int cand_lo,
+                                              int16_t* out, uint32_t* lds) {
+  const int lane = threadIdx.x & 63;
+  float hi = -INFINITY, lo = INFINITY;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const bool in = 64 * i + lane < C;
+    odd |= x[i] != x[i];
+    hi = in ? fmaxf(hi, x[i]) : hi;
+    lo = in ? fminf(lo, x[i]) : lo;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    hi = fmaxf(hi, __shfl_xor(hi, d, 64));
+    lo = fminf(lo, __shfl_xor(lo, d, 64));
+  }
+  const float scale = 256.f / (hi - lo);
+  if (__ballot(odd) != 0ull || !(hi > lo) || !(hi < INFINITY) || !(lo > -INFINITY) || !(scale < INFINITY)) return false;
+  auto bin = [&](float v) { return min((int)((v - lo) * scale), 255); };
+  *reinterpret_cast<uint4*>(&lds[4 * lane]) = make_uint4(0u, 0u, 0u, 0u);
+  wave_lds_sync();
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (64 * i + lane < C) atomicAdd(&lds[255 - bin(x[i])], 1u);  // slot 0: the highest bin
+  wave_lds_sync();
+  const uint4 c = *reinterpret_cast<const uint4*>(&lds[4 * lane]);
+  const int mine = (int)(c.x + c.y + c.z + c.w), incl = wave_incl_scan_dpp(mine);
+  const int at = (int)__builtin_ctzll(__ballot(incl >= n));  // n < C: there is one
+  int above = readlane_i(incl - mine, at), slot = 4 * at;    // scores in the bins before slot
+  const int c0 = readlane_i((int)c.x, at), c1 = readlane_i((int)c.y, at), c2 = readlane_i((int)c.z, at), c3 = readlane_i((int)c.w, at);
+  int count = c0;
+  if (above + count < n) { above += count; count = c1; ++slot; }
+  if (above + count < n) { above += count; count = c2; ++slot; }
+  if (above + count < n) { above += count; count = c3; ++slot; }
+  if (count > 64) return false;
+  wave_lds_sync();
+  // the bin's scores, one per lane, in index order
+  const int tb = 255 - slot;
+  int base = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const bool hit = 64 * i + lane < C && bin(x[i]) == tb;
+    const uint64_t b = __ballot(hit);
+    if (b == 0ull) continue;
+    if (hit) {
+      const int z = base + mbcnt64(b);
+      lds[z] = __float_as_uint(x[i]);
+      lds[64 + z] = (uint32_t)(64 * i + lane);
+    }
+    base += (int)__popcll(b);
+  }
+  wave_lds_sync();
+  const float k = __uint_as_float(lds[min(lane, count - 1)]);
+  const int idx = (int)lds[64 + min(lane, count - 1)];
+  int rank = 0;  // scores of the bin that come first: larger, or equal at a lower index (lanes are in index order)
+  for (int j = 0; j < count; ++j) {
+    const float o = readlane_f(k, j);
+    rank += o > k || (o == k && j < lane) ? 1 : 0;
+  }
+  const int last = (int)__builtin_ctzll(__ballot(lane < count && rank == n - above - 1));
+  const float kk = readlane_f(k, last);
+  const int ki = readlane_i(idx, last);
+  // everything above (kk, ki), in index order
+  int done = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const bool pick = 64 * i + lane < C && (x[i] > kk || (x[i] == kk && 64 * i + lane <= ki));
+    const uint64_t b = __ballot(pick);
+    if (b == 0ull) continue;
+    if (pick) out[done + mbcnt64(b)] = (int16_t)(cand_lo + 64 * i + lane);
+    done += (int)__popcll(b);
+  }
+  return true;
+}
+
 // One wavefront per node: forced blocks, padding, count, and the exact top-k over its block scores, in
 // registers up to 64 R candidates (R = 0: radix passes over the workspace).
 template <int R>
-__global__ __launch_bounds__(256) void tree_topk_kernel(TreeSelectArgs a, int64_t n_rows) {
-  __shared__ __align__(16) uint32_t lds[4][R == 0 ? 256 : 64];
+__global__ __launch_bounds__(256, R <= 32 ? 4 : 2) void tree_topk_kernel(TreeSelectArgs a, int64_t n_rows) {
+  __shared__ __align__(16) uint32_t lds[4][R == 1 ? 64 : 256];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t row = (int64_t)blockIdx.x * 4 + wave;
   if (row >= n_rows) return;
@@ -188,25 +270,21 @@ __global__ __launch_bounds__(256) void tree_topk_kernel(TreeSelectArgs a, int64_
   if constexpr (R == 0) {
     wave_topk_emit([&](int i) { return score_key(sc[i]); }, C, n, g.cand_lo, lds[wave], out);
   } else {
-    // slots past the candidates: key 0, below every score; the loads are requested before the first is
-    // waited for (the empty asm keeps each out of a branch of its own)
-    uint32_t key[R];
-    constexpr int kBatch = R < 16 ? R : 16;
+    // slots past the candidates repeat the last; the loads are requested before the first is waited for (the empty
+    // asm keeps each out of a branch of its own)
+    float x[R];
 #pragma unroll
-    for (int i0 = 0; i0 < R; i0 += kBatch) {
-      float x[kBatch];
+    for (int i = 0; i < R; ++i) x[i] = sc[min(64 * i + lane, C - 1)];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) x[i] = sc[min(64 * (i0 + i) + lane, C - 1)];
+    for (int i = 0; i < R; ++i) __asm__ __volatile__("" : "+v"(x[i]));
+    if constexpr (R == 1) {
+      lane_topk_emit(lane < C ? score_key(x[0]) : 0u, C, n, g.cand_lo, out);
+    } else if (!bin_topk_emit<R>(x, C, n, g.cand_lo, out, lds[wave])) {
+      uint32_t key[R];  // 0, below every score, past the candidates
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        __asm__ __volatile__("" : "+v"(x[i]));
-        key[i0 + i] = 64 * (i0 + i) + lane < C ? score_key(x[i]) : 0u;
-      }
-    }
-    if constexpr (R == 1)
-      lane_topk_emit(key[0], C, n, g.cand_lo, out);
-    else
+      for (int i = 0; i < R; ++i) key[i] = 64 * i + lane < C ? score_key(x[i]) : 0u;
       reg_topk_emit<R, true>(key, C, n, g.cand_lo, out, lds[wave]);
+    }
   }
 }
 

@@ -21,7 +21,10 @@ namespace {
 // Wavefronts of a workgroup: with q more of them, for the sums of whole rows inside the walk.
 template <bool kQ>
 constexpr int kWalkWaves = kQ ? 16 : 8;
-constexpr int kPickPieces = 16;              // most pieces that one workgroup takes from walk to token
+// Most pieces that one workgroup takes from walk to token (its wavefronts twice): the second launch costs the caller
+// 2 us, further pieces in turn more (18 nodes of one sequence without q: 32 pieces 9.0 us against 8.4, 63 pieces 12.1).
+template <bool kQ>
+constexpr int kPickPieces = kQ ? 32 : 16;
 constexpr int kPerLane = kVerifyPiece / 64;  // consecutive tokens of a piece that a lane holds
 
 // What the walk leaves for the pick.
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(64 * kWalkWaves<kQ>) void tree_walk_kernel(TreeVeri
   __shared__ double cs[NW][64];   // each wavefront's copy
   __shared__ double part[NW];
   __shared__ uint32_t gone[NW][kVerifyPiece / 32];
-  __shared__ double piece_sums[kPick ? 2 * kPickPieces : 2];
+  __shared__ double piece_sums[kPick ? 2 * kPickPieces<kQ> : 2];
   __shared__ int slots[64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int b = blockIdx.y, n = a.n;
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(64) void tree_pick_kernel(TreeVerifyArgs a, int n_p
 template <bool kBf16, bool kQ>
 hipError_t launch_verify(const TreeVerifyArgs& a, hipStream_t stream) {
   const int n_pieces = tree_verify_pieces(a.vocab);
-  if (n_pieces <= kPickPieces) {
+  if (n_pieces <= kPickPieces<kQ>) {
     hipLaunchKernelGGL((tree_walk_kernel<kBf16, kQ, true>), dim3(1, (unsigned)a.batch), dim3(64 * kWalkWaves<kQ>), 0, stream, a,
                        n_pieces);
     return hipGetLastError();

@@ -97,6 +97,46 @@ def test_select(dev, case, flat):
     assert torch.equal(sel.cpu(), want_sel)
 
 
+@pytest.mark.parametrize("t", [9000, 30000, 60000, 131000])
+@pytest.mark.parametrize("values", ["two", "steps", "tail", "nan", "inf"])
+def test_select_of_awkward_scores(dev, t, values):
+    """Scores that share few values, that lie far apart, that are not finite: the best by (score, lower block)."""
+    gen, rng = torch.Generator().manual_seed(t), random.Random(t)
+    n, k = 6, 64
+    s = shape_of(1, 1, 1, k, t, n)
+    f = torch.zeros(1, 1, n, D, dtype=torch.bfloat16)
+    f[..., 0] = 1  # a block's score is the first element of its key
+    kc = torch.zeros(1, 1, s.nc_cap, D, dtype=torch.bfloat16)
+    x = torch.randn(s.nc_cap, generator=gen)
+    if values == "two":
+        x = (x > 1.2).float()
+    elif values == "steps":
+        x = (x * 2).round()
+    elif values == "tail":
+        x[torch.rand(s.nc_cap, generator=gen) < 0.01] *= 2.0 ** 60
+    elif values == "inf":
+        x[torch.rand(s.nc_cap, generator=gen) < 0.02] = float("inf")
+        x[torch.rand(s.nc_cap, generator=gen) < 0.02] = -float("inf")
+    kc[0, 0, :, 0] = x.to(torch.bfloat16)
+    parent = trees(rng, 1, n, "wide")
+    want = ref.select(f, kc, [t], parent, k, 1, 2, (64, 64))
+    if values == "nan":  # what is chosen then is open; every entry is a block, each once
+        kc[0, 0, 5::7, 0] = NAN
+    sel = torch.full((1, 1, n + 1, k), 99, dtype=torch.int16, device=dev)
+    cnt = torch.full((1, 1, n), 99, dtype=torch.int16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_SELECT, n, t))
+    sp.sparda_tree_select(s, f.to(dev), n, torch.tensor([t], dtype=torch.int32, device=dev), t, parent.to(dev),
+                          kc.to(dev), sel, cnt, ws)
+    torch.cuda.synchronize()
+    assert bool((sel[:, :, n] == 99).all())
+    got = sel[:, :, :n].cpu()
+    assert torch.equal(cnt.cpu(), want[1])
+    if values == "nan":
+        assert bool((got[..., 1:] > got[..., :-1]).all()) and int(got.max()) <= (t + n) // L and int(got.min()) == 0
+    else:
+        assert torch.equal(got, want[0])
+
+
 def test_select_longer_contexts_count_as_t_max(dev):
     gen, rng = torch.Generator().manual_seed(7), random.Random(7)
     s = shape_of(2, 1, 1, 6, 1000, 5)
