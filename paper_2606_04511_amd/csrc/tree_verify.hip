@@ -67,45 +67,50 @@ __device__ __forceinline__ int row_shift(const void* base, int64_t at) {
   return (int)((reinterpret_cast<uintptr_t>(base) / (kBf16 ? 2 : 4) + (uintptr_t)at) & 3);
 }
 
-// The kPerLane elements of a row from e on, of which those outside [0, vocab) are 0; e plus the row's shift is a
-// multiple of 4.  One branch, so that all the loads of a lane inside the row are in flight together.
+// The kPerLane elements of a row from e on as they lie in memory, 0 for those outside [0, vocab); e plus the row's
+// shift is a multiple of 4.  They are converted by weight() afterwards, so that the loads of several rows are in flight
+// together.
 template <bool kBf16>
-__device__ __forceinline__ void load_piece(const void* base, int64_t row, int64_t e, int vocab, double* x) {
-  if (e >= 0 && e + kPerLane <= vocab) {
-    if constexpr (kBf16) {
-      uint2 w[kPerLane / 4];
+struct RawPiece {
+  uint32_t w[kBf16 ? kPerLane / 2 : kPerLane];
+
+  __device__ __forceinline__ void load(const void* base, int64_t row, int64_t e, int vocab) {
+    if (e >= 0 && e + kPerLane <= vocab) {
+      if constexpr (kBf16) {
+        const uint2* src = reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row + e);
 #pragma unroll
-      for (int k = 0; k < kPerLane / 4; ++k)
-        w[k] = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row + e + 4 * k);
+        for (int k = 0; k < kPerLane / 4; ++k) {
+          const uint2 v = src[k];
+          w[2 * k] = v.x;
+          w[2 * k + 1] = v.y;
+        }
+      } else {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(base) + row + e);
 #pragma unroll
-      for (int k = 0; k < kPerLane / 4; ++k) {
-        x[4 * k] = weight_of(bf16lo(w[k].x));
-        x[4 * k + 1] = weight_of(bf16hi(w[k].x));
-        x[4 * k + 2] = weight_of(bf16lo(w[k].y));
-        x[4 * k + 3] = weight_of(bf16hi(w[k].y));
+        for (int k = 0; k < kPerLane / 4; ++k) {
+          const uint4 v = src[k];
+          w[4 * k] = v.x;
+          w[4 * k + 1] = v.y;
+          w[4 * k + 2] = v.z;
+          w[4 * k + 3] = v.w;
+        }
       }
     } else {
-      float4 w[kPerLane / 4];
+      auto at = [&](int k) -> uint32_t {
+        const bool in = e + k >= 0 && e + k < vocab;
+        const int64_t from = row + (in ? e + k : 0);
+        const uint32_t v = kBf16 ? (uint32_t) static_cast<const uint16_t*>(base)[from] : static_cast<const uint32_t*>(base)[from];
+        return in ? v : 0u;
+      };
 #pragma unroll
-      for (int k = 0; k < kPerLane / 4; ++k)
-        w[k] = *reinterpret_cast<const float4*>(static_cast<const float*>(base) + row + e + 4 * k);
-#pragma unroll
-      for (int k = 0; k < kPerLane / 4; ++k) {
-        x[4 * k] = weight_of(w[k].x);
-        x[4 * k + 1] = weight_of(w[k].y);
-        x[4 * k + 2] = weight_of(w[k].z);
-        x[4 * k + 3] = weight_of(w[k].w);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) {
-      const bool in = e + k >= 0 && e + k < vocab;
-      const double y = prob_at<kBf16>(base, row + (in ? e + k : 0));
-      x[k] = in ? y : 0.0;
+      for (int k = 0; k < (kBf16 ? kPerLane / 2 : kPerLane); ++k) w[k] = kBf16 ? at(2 * k) | at(2 * k + 1) << 16 : at(k);
     }
   }
-}
+  __device__ __forceinline__ double weight(int k) const {
+    if constexpr (kBf16) return weight_of(k & 1 ? bf16hi(w[k / 2]) : bf16lo(w[k / 2]));
+    return weight_of(__uint_as_float(w[k]));
+  }
+};
 
 // What `rounds` rejections with q leave of weight m; each product and difference is rounded by itself.
 __device__ __forceinline__ double left_of(double m, double q, const double* c, int rounds) {
@@ -123,10 +128,20 @@ __device__ __forceinline__ double readlane_d(double x, int lane) {
   return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
 }
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)u), hi = (uint32_t)dpp_i<CTRL>((int)(u >> 32));
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+
+// Sum over the wavefront, the same bits in every lane: rotations inside the rows of 16 lanes, then the four rows.
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
-  return x;
+  x += dpp_d<0x128>(x);  // row_ror:8
+  x += dpp_d<0x124>(x);
+  x += dpp_d<0x122>(x);
+  x += dpp_d<0x121>(x);
+  return (readlane_d(x, 0) + readlane_d(x, 16)) + (readlane_d(x, 32) + readlane_d(x, 48));
 }
 
 // Sum over the workgroup, the same bits in every thread; `part` holds one double per wavefront.
@@ -141,8 +156,6 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
   for (int w = 0; w < NW; ++w) s += part[w];
   return s;
 }
-
-__device__ __forceinline__ double readlane_sum(double x) { return readlane_d(wave_sum(x), 0); }
 
 // Inclusive running sum over the wavefront's lanes.
 __device__ __forceinline__ double wave_scan(double x) {
@@ -168,11 +181,16 @@ __device__ __forceinline__ void piece_weights(const TreeVerifyArgs& a, int64_t r
     for (int k = 0; k < kPerLane; ++k) s += x[k];
     return s;
   };
-  load_piece<kBf16>(a.p, row, e0 + kPerLane * lane, a.vocab, x);
+  RawPiece<kBf16> rp, rq;
+  if (kQ && rounds > 0) rq.load(a.q, row, e0 + kPerLane * lane, a.vocab);
+  rp.load(a.p, row, e0 + kPerLane * lane, a.vocab);
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) x[k] = rp.weight(k);
   if constexpr (kQ) {
     if (rounds > 0) {
       double y[kPerLane];
-      load_piece<kBf16>(a.q, row, e0 + kPerLane * lane, a.vocab, y);
+#pragma unroll
+      for (int k = 0; k < kPerLane; ++k) y[k] = rq.weight(k);
 #pragma unroll 1
       for (int r = 0; r < rounds; ++r) {
         if (before && r + 1 == rounds) *before = sum();
@@ -199,8 +217,8 @@ __device__ __forceinline__ int pick_token(const TreeVerifyArgs& a, int b, const 
     s1 += sums[2 * i];
     s0 += sums[2 * i + 1];
   }
-  s1 = readlane_sum(s1);
-  s0 = readlane_sum(s0);
+  s1 = wave_sum(s1);
+  s0 = wave_sum(s0);
   const int undone = s1 > 0.0 ? 0 : 1;  // the last rejection left nothing: it does not count
   const double total = undone ? s0 : s1;
   if (!(total > 0.0)) return -1;
