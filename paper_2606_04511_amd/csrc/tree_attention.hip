@@ -234,7 +234,8 @@ struct TreeCols {
 
   // One half block: K rows at kbuf, V rows at vbuf (rows of 256 bytes, 16-byte piece x of token t at x ^ (t % 16) for K
   // and x ^ 2 (t % 8) for V).  valid: its tokens that hold a V; they are the context's, or the drafted ones from node
-  // 32 hf on.  k_read runs once K has been read, v_ready before V is, v_read after.
+  // 32 hf on.  k_read runs once K has been read, v_ready before V is; kVFirst: V is there already and is read before the
+  // softmax.
   template <bool kVFirst, class KRead, class VReady>
   __device__ __forceinline__ void half(const char* kbuf, const char* vbuf, bool tree, int hf, int e, uint32_t valid,
                                        KRead k_read, VReady v_ready) {
