@@ -160,11 +160,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _stream(stream):
     if stream is None:
-        if not torch.cuda.is_available():
-            return 0
-        if _raw_stream is not None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
             return _raw_stream(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
