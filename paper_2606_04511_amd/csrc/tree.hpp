@@ -116,6 +116,8 @@ struct TreeAttnPlan {
 // nodes 144 and 114), of 256 groups 110 and 94.
 // With fewer workgroups than CUs the blocks are split over them: at least half a block per wavefront, or three blocks
 // per workgroup where the wavefronts share them (one each: 19 -> 24 us for 22 nodes of 3 groups of 4 heads, 55 blocks).
+// The second launch reads up to 8 splits at once: beyond 16 the finer split of lists that differ by node costs what it
+// saves (7 nodes of 4 groups, 64 blocks: 16 splits 18.9 us, 33 20.1).
 inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size, int32_t k_total, int64_t t_max,
                                    bool one_list) {
   TreeAttnPlan p;
@@ -131,7 +133,11 @@ inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size
     p.width = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
   const int64_t wgs = groups * ((cols + p.width - 1) / p.width), blocks = at_most(k_total);
   int64_t ns = 256 / wgs;
-  const int64_t most = p.width <= 32 ? (2 * blocks + 2 + 7) / 8 : (blocks + 1 + 2) / 3;
+  int64_t most = p.width <= 32 ? (2 * blocks + 2 + 7) / 8 : (blocks + 1 + 2) / 3;
+  if (p.width <= 32 && !one_list && n > 1) {  // about twice the blocks: up to 16 splits for them
+    const int64_t twice = (2 * at_most(2 * (int64_t)k_total) + 2 + 7) / 8, some = twice < 16 ? twice : 16;
+    most = most > some ? most : some;
+  }
   ns = ns < most ? ns : most;
   ns = ns > 64 ? 64 : ns < 1 ? 1 : ns;
   p.n_splits = (int32_t)ns;
