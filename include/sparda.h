@@ -428,7 +428,8 @@ int sparda_tree_select(const sparda_shape* shape, const void* f, int32_t n_nodes
  *   o      out : bf16 [B][Hq][n_nodes][D] device; zeros for an absent node or sequence.
  *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_TREE_ATTN).
  * o_i = softmax(sm_scale q_i K^T) V over the tokens t < t_ctx of node i's blocks and the tokens of
- * A(i): bf16 inputs, float32 accumulation and online softmax.  Whatever the caches hold from t_ctx
+ * A(i): bf16 inputs, float32 accumulation and online softmax; a weight enters the product with V to
+ * within 2^-16 of itself.  Whatever the caches hold from t_ctx
  * on, and whatever lies in the rows of absent nodes, has no effect.  The V of a block that any node
  * of a tree lists, and of its present nodes, has to be finite: a matrix product serves several nodes,
  * and those that do not attend a row meet it with weight 0.

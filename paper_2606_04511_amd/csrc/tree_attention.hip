@@ -18,15 +18,18 @@
 //   3. Per half and 16 columns: S^T = K Q^T on v_mfma_f32_16x16x32_bf16 (lane (c, g) holds column c's
 //      scores of tokens 16 tt + 4 g + i); masks; P = 2^(z - m) with a reference m that moves only when a
 //      score exceeds it by more than 2^8; O^T += V^T P^T on the same MFMA, V read through the transposing
-//      LDS read.  The denominators sum P in float32, before it is rounded to bf16 for the product (a
-//      weight is off by at most 2^-8 of itself).
+//      LDS read.  P enters the product as two bf16 numbers, itself rounded and what that rounding took, so
+//      a weight is off by at most 2^-16 of itself; the denominators sum it in float32.  With the rounded
+//      one alone (2^-8) the products take half the instructions (27 nodes of 64 groups below: 89 us instead
+//      of 100; 16 nodes of 256 groups 90.5 and 92.5), but a step over a tree would be less exact than the
+//      decode steps it stands for.
 //   4. The wavefronts' states merge through LDS; with splits their float32 partials go to the workspace
 //      and a second launch merges them.
 //
 // What bounds it.  16 nodes of 256 groups of 4 heads at 128K, 64 blocks (537 MB): 91 us, 5.9 TB/s, the memory's rate
-// with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 93 us, of which 9 before the
-// first product, 3 after the last; each of the 48 blocks of a workgroup takes 1.7 us, three blocks' loads in flight.
-// 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 100-116 us, a block read from L2 once per two nodes
+// with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 100 us, of which 9 before the
+// first product, 3 after the last; each of the 48 blocks of a workgroup takes 1.8 us, three blocks' loads in flight.
+// 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 123 us, a block read from L2 once per two nodes
 // (256 columns per workgroup: 143, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 13
 // us and 4 for the merge of the splits, a chain of latencies.
 #include <math.h>
@@ -314,20 +317,24 @@ struct TreeCols {
         }
       }
     }
-    bf16x8 pb[NT];
+    bf16x8 pb[NT], pr[NT];  // the weights rounded to bf16, and what the rounding took, rounded likewise
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (!on[nt]) continue;
-      float p[2][4];
+      uint32_t big[4], rest[4];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+      for (int x = 0; x < 4; ++x) {
+        float p[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[tt][i] = __builtin_amdgcn_exp2f(fmaf(st[nt][tt][i], zscale, off[nt]));
-          l[nt] += p[tt][i];
+        for (int i = 0; i < 2; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(st[nt][x >> 1][2 * (x & 1) + i], zscale, off[nt]));
+          l[nt] += p[i];
         }
-      pb[nt] = as_bf16x8(make_uint4(pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]),
-                                    pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])));
+        big[x] = pack_bf16(p[0], p[1]);
+        rest[x] = pack_bf16(p[0] - bf16lo(big[x]), p[1] - bf16hi(big[x]));
+      }
+      pb[nt] = as_bf16x8(make_uint4(big[0], big[1], big[2], big[3]));
+      pr[nt] = as_bf16x8(make_uint4(rest[0], rest[1], rest[2], rest[3]));
     }
     if constexpr (!kVFirst) {
       v_ready();
@@ -336,6 +343,8 @@ struct TreeCols {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (!on[nt]) continue;
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) o[nt][dt] = mfma16x16x32(vf[dt], pr[nt], o[nt][dt]);
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) o[nt][dt] = mfma16x16x32(vf[dt], pb[nt], o[nt][dt]);
     }
