@@ -51,7 +51,7 @@ constexpr int kTaBuf = kTaHalf * kHeadDim * 2;       // bytes of a half's K or V
 constexpr int kTaSlot = 4 * kTaBuf;                  // bytes of a block's K, then its V
 constexpr int kTaRing = 4;                           // blocks in LDS at once (shared form)
 constexpr int kTaWindow = 2048;                      // blocks per window of the table
-constexpr int kTaTree = 0x7fff;                      // the list's entry of the drafted tokens
+constexpr int kTaTree = -1;                          // the list's entry of the drafted tokens: no block has this number
 constexpr int kTaPitch = kHeadDim + 4;               // floats per merged row: 16 rows of 16 bytes touch every bank once
 constexpr int kTaPartial = kHeadDim + 4;             // floats of a split's partial: m, l, two unused, the sums
 constexpr int kCombineThreads = 256;

@@ -1,12 +1,61 @@
 """The operators over trees of drafted tokens where their results are most delicate, against the definitions in
 float64 (tree_reference.py)."""
+import random
+
 import pytest
 import torch
 
+import paper_2606_04511_amd.sparda as sp
 import tree_reference as ref
-from test_gpu_tree import ATTN, attn_inputs, dev, run_attn, say  # noqa: F401
+from test_gpu_tree import ATTN, D, L, NAN, attn_inputs, dev, run_attn, say, shape_of, trees, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+# ---- attention: the last block of the largest cache ------------------------------------------------------
+
+LAST = [
+    # nodes, group, entries per list, one list: 16 columns; 32; 64 of wavefronts that share the blocks (the split of the
+    # work goes by the entries that a list may hold, not by those it holds)
+    (1, 4, 6, False),
+    (8, 4, 6, False),
+    (9, 4, 8192, True),
+    (17, 4, 8192, False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(LAST)))
+def test_attn_last_block_of_the_largest_cache(dev, case):  # noqa: F811
+    """32768 blocks are the most that a cache can have; the last one, number 32767, is a block as any other."""
+    n, G, k, shared = LAST[case]
+    say("tree attention at 2097152 tokens", LAST[case])
+    gen, rng = torch.Generator().manual_seed(case), random.Random(case)
+    t_cap = 32768 * L
+    t = t_cap - n  # the last block holds 64 - n tokens
+    s = shape_of(1, 1, G, k, t, n, t_cap=t_cap)
+    blocks = [0, 100, 30720, 32766, 32767]
+    rows = torch.cat([torch.arange(j * L, min(j * L + L, t)) for j in blocks])
+    caches = []
+    for _ in range(2):  # NaN in what no list names and from t on
+        x = torch.full((1, 1, t_cap, D), NAN, dtype=torch.bfloat16, device=dev)
+        x[0, 0, rows.to(dev)] = torch.randn(len(rows), D, generator=gen).to(torch.bfloat16).to(dev)
+        caches.append(x)
+    q, kt, vt = (torch.randn(1, h, n, D, generator=gen).to(torch.bfloat16) for h in (G, 1, 1))
+    parent = trees(rng, 1, n, "wide")
+    ns = 1 if shared else n
+    sel, cnt = torch.full((1, 1, ns, k), -1, dtype=torch.int16), torch.full((1, 1, ns), 5, dtype=torch.int16)
+    for i in range(ns):
+        sel[0, 0, i, :5] = torch.tensor(rng.sample(blocks, 5), dtype=torch.int16)
+        cnt[0, 0, i] = 5 if i % 3 < 2 else 3
+    o = torch.full(q.shape, NAN, dtype=torch.bfloat16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_ATTN, n, t))
+    sp.sparda_tree_attn(s, q.to(dev), n, torch.tensor([t], dtype=torch.int32, device=dev), t, parent.to(dev), *caches,
+                        kt.to(dev), vt.to(dev), ns, sel.to(dev), cnt.to(dev), ref.SCALE, o, ws)
+    torch.cuda.synchronize()
+    want, w = ref.attn(q, *(x.cpu() for x in caches), kt, vt, [t], parent, sel, cnt, ref.SCALE)
+    assert not torch.isnan(want).any()
+    off = (o.cpu().double() - want).abs()
+    assert bool((off <= ref.attn_bar(want, w)).all())
 
 
 # ---- attention: weights that must cancel --------------------------------------------------------------------
