@@ -400,8 +400,9 @@ int sparda_writeback_kv(const sparda_shape* shape, const void* k_new, const void
  * sparda_tree_select -- the attended block set of every node (Sec. 4.1, Eq. 4; Eq. 1), as
  * sparda_forecast_select gives it for a row at the node's position.
  *   f      in  : bf16 [B][Hkv][n_nodes][D] device, the nodes' Forecast rows.
- *   k_cmp  in  : bf16 [B][Hkv][nc_cap][D] device; every window complete within a sequence's t_ctx
- *                tokens must be valid; the last one that can be scored must be < nc_cap.
+ *   k_cmp  in  : bf16 [B][Hkv][nc_cap][D] device; every window that overlaps a candidate block and is
+ *                complete within the sequence's t_ctx tokens must be valid and < nc_cap, the candidates
+ *                being those of a node at position t_ctx + n_nodes - 1; no later window is read.
  *   sel    out : int16 [B][Hkv][n_nodes][k_total] device: ascending block indices, -1 padded.
  *   cnt    out : int16 [B][Hkv][n_nodes] device; 0 (and all -1) for an absent node or sequence.
  *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_TREE_SELECT).

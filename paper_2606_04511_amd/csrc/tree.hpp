@@ -99,6 +99,21 @@ inline size_t tree_select_ws(int64_t groups, int64_t t_max, int32_t n, int32_t n
   return (size_t)groups * n * (size_t)tree_select_stride(t_max, n, n_init, n_local) * sizeof(float);
 }
 
+// The last compressed key that the selection of a context of t tokens reads: of the windows that overlap a candidate of
+// the deepest node there can be, the last one complete within t.  -1: no key is read.  It does not fall as t grows.
+__host__ __device__ inline int32_t tree_last_key(const WinGrid& grid, int64_t t, int32_t n, int32_t n_init,
+                                                 int32_t n_local, int32_t k_total) {
+  const RowGeom g = row_geom(t + n - 1, n_init, n_local, k_total);
+  if (g.n_cand <= 0) return -1;
+  const int32_t hi = grid_win_hi(grid, g.cand_lo + g.n_cand - 1), vis = grid_win_vis(grid, t - 1);
+  return hi < vis ? hi : vis;
+}
+// The row read for window w: those before the first and past the last are requested too (a step is 64 keys).
+__host__ __device__ inline int32_t tree_key_row(int32_t w, int32_t last) {
+  const int32_t x = w < last ? w : last;
+  return x > 0 ? x : 0;
+}
+
 // How an attention call is cut into workgroups, one of which fits a CU.
 struct TreeAttnPlan {
   int32_t width;     // columns (node, query head) of a workgroup: 16 or 32, whose wavefronts stream blocks of

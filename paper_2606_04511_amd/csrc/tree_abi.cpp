@@ -39,15 +39,9 @@ int sparda_tree_select(const sparda_shape* shape, const void* f, int32_t n_nodes
   if (shape->n_local < 2)
     return fail(SPARDA_ERR_UNSUPPORTED, "n_local %d < 2: the block that drafted tokens complete has no compressed key",
                 shape->n_local);
-  // the last key that the deepest node of the longest context could score
-  const sparda::RowGeom g = sparda::row_geom(t_max + n_nodes - 1, shape->n_init, shape->n_local, shape->k_total);
-  if (g.n_cand > 0) {
-    const int32_t hi = sparda::grid_win_hi(grid_of(shape), g.cand_lo + g.n_cand - 1);
-    const int32_t vis = sparda::grid_win_vis(grid_of(shape), t_max - 1);
-    const int32_t last = hi < vis ? hi : vis;
-    if (last >= shape->nc_cap)
-      return fail(SPARDA_ERR_INVALID_ARG, "compressed key %d beyond nc_cap %lld", last, (long long)shape->nc_cap);
-  }
+  const int32_t last = sparda::tree_last_key(grid_of(shape), t_max, n_nodes, shape->n_init, shape->n_local, shape->k_total);
+  if (last >= shape->nc_cap)
+    return fail(SPARDA_ERR_INVALID_ARG, "compressed key %d beyond nc_cap %lld", last, (long long)shape->nc_cap);
   const int64_t groups = (int64_t)shape->batch * shape->n_kv_heads;
   const size_t need = sparda::tree_select_ws(groups, t_max, n_nodes, shape->n_init, shape->n_local);
   if (need > 0) {

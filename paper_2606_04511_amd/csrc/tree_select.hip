@@ -53,7 +53,8 @@ __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n
   const int x_end = min(g.n_cand, (part + 1) * steps * kPerStep);
   int x0 = part * steps * kPerStep;
   if (x0 >= x_end) return;
-  const int32_t vis = grid_win_vis(a.grid, t - 1);  // nothing past it is read
+  const int32_t vis = grid_win_vis(a.grid, t - 1);
+  const int32_t last_key = tree_last_key(a.grid, t, n, a.n_init, a.n_local, a.k_total);  // nothing past it is read
   bf16x8 fa[MT][4];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n
     for (int ks = 0; ks < 4; ++ks) fa[mt][ks] = as_bf16x8(ld16(src + 32 * ks));
   }
   const uint16_t* keys = a.kc + bm * a.nc_cap * kHeadDim + 8 * q;
-  auto key_at = [&](int w) { return keys + (int64_t)max(min(w, vis), 0) * kHeadDim; };
+  auto key_at = [&](int w) { return keys + (int64_t)tree_key_row(w, last_key) * kHeadDim; };
   auto products = [&](const uint4* kw, int mt) {
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void tree_score_kernel(TreeSelectArgs a, int n
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int z = 4 * i + r4, col = kBlocks ? z & 15 : i;
-      lds_load16<true>(rows, (uint32_t)max(min(w0 + z, vis), 0) * 256 + 16 * ((lane & 15) ^ col), buf_at + 1024 * i);
+      lds_load16<true>(rows, (uint32_t)tree_key_row(w0 + z, last_key) * 256 + 16 * ((lane & 15) ^ col), buf_at + 1024 * i);
     }
   };
   request(x0);

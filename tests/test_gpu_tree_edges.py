@@ -7,7 +7,8 @@ import torch
 
 import paper_2606_04511_amd.sparda as sp
 import tree_reference as ref
-from test_gpu_tree import ATTN, D, L, NAN, attn_inputs, dev, run_attn, say, shape_of, trees, workspace  # noqa: F401
+from test_gpu_tree import (ATTN, D, L, NAN, attn_inputs, dev, exact_rows, run_attn, say, shape_of, trees,  # noqa: F401
+                           workspace)
 
 pytestmark = pytest.mark.gpu
 
@@ -87,3 +88,43 @@ def test_attn_weights_keep_their_bits(dev, case):  # noqa: F811
     worst = float((off / fine_bar(want, w, z, terms)).max())
     say(f"  logits up to {z:.2f}, worst error {worst:.3f} of the bar")
     assert worst <= 1.0
+
+
+# ---- select: the smallest cache of compressed keys -----------------------------------------------------------
+
+SMALL_KC = [
+    # t_ctx per sequence, nodes, kv heads, k, n_init, n_local, grid
+    ((4096,), 1, 1, 40, 1, 32, (64, 64)),
+    ((4096, 3000, 2111), 8, 2, 40, 1, 32, (64, 64)),
+    ((9000, 8192), 64, 1, 12, 0, 5, (64, 64)),
+    ((4000, 3999), 5, 2, 9, 1, 2, (32, 16)),
+    ((4111, 4111), 33, 1, 50, 2, 40, (32, 16)),
+    ((2000,), 20, 3, 12, 0, 9, (32, 16)),
+]
+
+
+@pytest.mark.parametrize("case", range(len(SMALL_KC)))
+def test_select_with_the_smallest_key_cache(dev, case):  # noqa: F811
+    """nc_cap is one more than the last window that can be scored; one less is refused.  The keys end with the tensor."""
+    t_ctx, n, H, k, n_init, n_local, grid = SMALL_KC[case]
+    say("tree select, smallest key cache", SMALL_KC[case])
+    gen, rng = torch.Generator().manual_seed(case), random.Random(case)
+    B, t_max, (l, st) = len(t_ctx), max(t_ctx), grid
+    last = min((t_max - l) // st, (((t_max + n - 1) // L - n_local + 1) * L - 1) // st)
+    s = shape_of(B, H, 1, k, t_max, n, n_init, n_local, grid)
+    assert last + 1 < s.nc_cap
+    s.nc_cap = last + 1
+    f, kc = exact_rows(gen, B, H, n, D), exact_rows(gen, B, H, last + 1, D)
+    parent = trees(rng, B, n, "wide" if case % 2 else "chain")
+    want = ref.select(f, kc, t_ctx, parent, k, n_init, n_local, grid)
+    sel = torch.full((B, H, n, k), 99, dtype=torch.int16, device=dev)
+    cnt = torch.full((B, H, n), 99, dtype=torch.int16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_SELECT, n, t_max))
+    args = (f.to(dev), n, torch.tensor(t_ctx, dtype=torch.int32, device=dev), t_max, parent.to(dev), kc.to(dev), sel, cnt, ws)
+    sp.sparda_tree_select(s, *args)
+    torch.cuda.synchronize()
+    assert torch.equal(sel.cpu(), want[0]) and torch.equal(cnt.cpu(), want[1])
+    s.nc_cap = last
+    with pytest.raises(sp.SpardaError) as ei:
+        sp.sparda_tree_select(s, *args)
+    assert ei.value.status == sp.SPARDA_ERR_INVALID_ARG
