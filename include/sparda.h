@@ -433,7 +433,8 @@ int sparda_tree_select(const sparda_shape* shape, const void* f, int32_t n_nodes
  * within 2^-16 of itself.  Whatever the caches hold from t_ctx
  * on, and whatever lies in the rows of absent nodes, has no effect.  The V of a block that any node
  * of a tree lists, and of its present nodes, has to be finite: a matrix product serves several nodes,
- * and those that do not attend a row meet it with weight 0.
+ * and those that do not attend a row meet it with weight 0.  A NaN in a node's query, or in a key
+ * that it attends, makes its output NaN.
  */
 int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, const int32_t* t_ctx, int64_t t_max,
                      const int32_t* parent, const void* k, const void* v, const void* k_tree, const void* v_tree,

@@ -365,13 +365,16 @@ __device__ __forceinline__ uint32_t half_valid(const TreeUnit& u, bool tree, int
   return left >= kTaHalf ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
 }
 
+// 1 / den; 0 for a column without a token, whose den is 0.  NaN stays NaN.
+__device__ __forceinline__ float inverse_of(float den) { return den == 0.f ? 0.f : 1.f / den; }
+
 // Four dims of a finished column, or of a split's partial.
 __device__ __forceinline__ void store_dims(const TreeAttnArgs& a, const TreeUnit& u, int c, int d, float m, float den,
                                            f32x4 num) {
   const int node = node_of(a, c);
   const int64_t row = (u.bm * a.group_size + (c - node * a.group_size)) * a.tb.n + node;
   if (a.n_splits == 1) {
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+    const float inv = inverse_of(den);
     uint2 w;
     w.x = (uint32_t)f32_to_bf16(num[0] * inv) | ((uint32_t)f32_to_bf16(num[1] * inv) << 16);
     w.y = (uint32_t)f32_to_bf16(num[2] * inv) | ((uint32_t)f32_to_bf16(num[3] * inv) << 16);
@@ -511,15 +514,16 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
       float m = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kTaWaves; ++w) m = fmaxf(m, st_m[w * 16 + cl]);
+      // a wavefront without a score has m = -inf and weighs nothing; one whose scores are all NaN has m = -inf too, and
+      // sums of NaN that reach the result
+      const float ref = m > -INFINITY ? m : 0.f;
       float den = 0.f;
       f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (m != -INFINITY) {
 #pragma unroll
-        for (int w = 0; w < kTaWaves; ++w) {
-          const float sc = __builtin_amdgcn_exp2f(st_m[w * 16 + cl] - m);  // 0 for a wavefront without a score
-          den = fmaf(st_l[w * 16 + cl], sc, den);
-          num += *reinterpret_cast<const f32x4*>(&st_o[(w * 16 + cl) * kTaPitch + d]) * sc;
-        }
+      for (int w = 0; w < kTaWaves; ++w) {
+        const float sc = __builtin_amdgcn_exp2f(st_m[w * 16 + cl] - ref);
+        den = fmaf(st_l[w * 16 + cl], sc, den);
+        num += *reinterpret_cast<const f32x4*>(&st_o[(w * 16 + cl) * kTaPitch + d]) * sc;
       }
       store_dims(a, u, c, d, m, den, num);
     }
@@ -669,22 +673,21 @@ __global__ __launch_bounds__(kCombineThreads) void tree_combine_kernel(TreeAttnA
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
-    if (top == -INFINITY) continue;
-    const float keep = __builtin_amdgcn_exp2f(m - top);
+    const float ref = top > -INFINITY ? top : 0.f;  // as in the merge of the wavefronts
+    const float keep = __builtin_amdgcn_exp2f(m - ref);
     l *= keep;
     o0 *= keep;
     o1 *= keep;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (ml[i].x == -INFINITY) continue;  // a split without a score weighs nothing
-      const float w = __builtin_amdgcn_exp2f(ml[i].x - top);
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - ref);
       l = fmaf(ml[i].y, w, l);
       o0 = fmaf(po[i].x, w, o0);
       o1 = fmaf(po[i].y, w, o1);
     }
     m = top;
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = inverse_of(l);
   reinterpret_cast<uint32_t*>(a.o + row * kHeadDim)[lane] = (uint32_t)f32_to_bf16(o0 * inv) | ((uint32_t)f32_to_bf16(o1 * inv) << 16);
 }
 

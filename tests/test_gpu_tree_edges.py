@@ -59,6 +59,85 @@ def test_attn_last_block_of_the_largest_cache(dev, case):  # noqa: F811
     assert bool((off <= ref.attn_bar(want, w)).all())
 
 
+# ---- attention: NaN in what a node attends ------------------------------------------------------------------
+
+# nodes, group, kv heads, batch, entries per list, t: 16 and 32 columns with splits and without, and the forms whose
+# wavefronts share the blocks (lists that may hold many entries), with splits and without
+SPREAD = [
+    (5, 3, 1, 2, 6, 700),
+    (7, 4, 2, 2, 8, 1500),
+    (3, 4, 64, 4, 6, 700),
+    (8, 4, 64, 4, 6, 700),
+    (13, 3, 1, 1, 9000, 600000),
+    (40, 4, 64, 4, 40, 2600),
+    (16, 4, 64, 4, 40, 2600),
+]
+
+
+def spread_inputs(dev, case):  # noqa: F811
+    n, G, H, B, k, t = SPREAD[case]
+    gen, rng = torch.Generator(device=dev).manual_seed(case), random.Random(case)
+    s = shape_of(B, H, G, k, t, n)
+    mk = lambda *size: torch.randn(*size, generator=gen, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    q, kk, vv = mk(B, H * G, n, D), mk(B, H, s.t_cap, D), mk(B, H, s.t_cap, D)
+    kt, vt = mk(B, H, n, D), mk(B, H, n, D)
+    parent = trees(rng, B, n, "wide")
+    nb, some = -(-t // L), 5
+    sel = torch.full((B, H, n, k), -1, dtype=torch.int16, device=dev)
+    sel[..., :some] = torch.rand(B, H, n, nb, generator=gen, device=dev).topk(some, dim=3).indices.to(torch.int16)
+    cnt = torch.full((B, H, n), some, dtype=torch.int16, device=dev)
+    return s, n, [t - 64 * b for b in range(B)], q, parent, kk, vv, kt, vt, sel, cnt
+
+
+def spread_call(dev, x):  # noqa: F811
+    s, n, t_ctx, q, parent, kk, vv, kt, vt, sel, cnt = x
+    t = torch.tensor(t_ctx, dtype=torch.int32, device=dev)
+    o = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_ATTN, n, max(t_ctx)))
+    sp.sparda_tree_attn(s, q, n, t, max(t_ctx), parent.to(dev), kk, vv, kt, vt, n, sel, cnt, ref.SCALE, o, ws)
+    torch.cuda.synchronize()
+    return o
+
+
+@pytest.mark.parametrize("what", ["query", "context key", "drafted key"])
+@pytest.mark.parametrize("case", range(len(SPREAD)))
+def test_attn_nan_reaches_those_that_attend_it(dev, case, what):  # noqa: F811
+    """A NaN in a node's query, or in a key that it attends, makes that node's output NaN, whatever the number of groups;
+    the other nodes' outputs stay as they are, bit for bit."""
+    say("tree attention, NaN in a", what, SPREAD[case])
+    x = spread_inputs(dev, case)
+    s, n, t_ctx, q, parent, kk, vv, kt, vt, sel, cnt = x
+    G = s.group_size
+    plain = spread_call(dev, x)
+    assert not torch.isnan(plain).any()
+    bad = torch.zeros(q.shape[:3], dtype=torch.bool)
+    for b in range(s.batch):
+        up = ref.paths(parent[b].tolist())
+        for h in {0, s.n_kv_heads // 2}:
+            node = (b + h) % n
+            if what == "query":
+                q[b, h * G + G - 1, node, 5] = NAN
+                bad[b, h * G + G - 1, node] = True
+            elif what == "drafted key":
+                kt[b, h, node, 77] = NAN
+                for i in range(n):
+                    bad[b, h * G:h * G + G, i] = node in up[i]
+            else:  # the last token of the context that the node's first entry holds
+                j = int(sel[b, h, node, 0])
+                tok = min(j * L + L, t_ctx[b]) - 1
+                if tok < j * L:
+                    continue
+                kk[b, h, tok, 0] = NAN
+                for i in range(n):
+                    bad[b, h * G:h * G + G, i] = j in sel[b, h, i, :int(cnt[b, h, i])].tolist()
+    assert bad.any()
+    got = spread_call(dev, x)
+    seen = torch.isnan(got).cpu()
+    assert torch.equal(seen.all(3), bad) and torch.equal(seen.any(3), bad)
+    keep = ~bad.to(dev)
+    assert torch.equal(got[keep].view(torch.int16), plain[keep].view(torch.int16))
+
+
 # ---- attention: weights that must cancel --------------------------------------------------------------------
 
 def fine_bar(o, w, z, terms):
