@@ -71,9 +71,9 @@ inline int check_dev(const void* p, const char* name, uintptr_t align) {
 
 inline int check_rows(const sparda_shape* s, int32_t n_q, int64_t q_pos0) {
   if (n_q < 1) return fail(SPARDA_ERR_INVALID_ARG, "n_q %d < 1", n_q);
-  if (q_pos0 < 0 || q_pos0 + n_q > s->t_cap)
-    return fail(SPARDA_ERR_INVALID_ARG, "positions [%lld, %lld) outside t_cap %lld", (long long)q_pos0,
-                (long long)(q_pos0 + n_q), (long long)s->t_cap);
+  if (q_pos0 < 0 || q_pos0 > s->t_cap - n_q)  // (q_pos0 + n_q can pass 64 bits)
+    return fail(SPARDA_ERR_INVALID_ARG, "%d positions from %lld on outside t_cap %lld", n_q, (long long)q_pos0,
+                (long long)s->t_cap);
   const int64_t rows = (int64_t)s->batch * s->n_kv_heads * n_q;
   if (rows > (int64_t)1 << 30) return fail(SPARDA_ERR_UNSUPPORTED, "too many query rows");
   return SPARDA_OK;

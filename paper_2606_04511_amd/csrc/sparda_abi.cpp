@@ -490,9 +490,9 @@ int sparda_writeback_kv(const sparda_shape* shape, const void* k_new, const void
       (rc = check_dev(host_k, "host_k", 16)) || (rc = check_dev(host_v, "host_v", 16)))
     return rc;
   if (n_new < 1) return fail(SPARDA_ERR_INVALID_ARG, "n_new %d < 1", n_new);
-  if (pos0 < 0 || pos0 + n_new > shape->t_cap)
-    return fail(SPARDA_ERR_INVALID_ARG, "positions [%lld, %lld) outside t_cap %lld", (long long)pos0,
-                (long long)(pos0 + n_new), (long long)shape->t_cap);
+  if (pos0 < 0 || pos0 > shape->t_cap - n_new)
+    return fail(SPARDA_ERR_INVALID_ARG, "%d positions from %lld on outside t_cap %lld", n_new, (long long)pos0,
+                (long long)shape->t_cap);
   if (n_workgroups < 1) return fail(SPARDA_ERR_INVALID_ARG, "n_workgroups %d < 1", n_workgroups);
   void* dk = nullptr;
   void* dv = nullptr;
