@@ -122,13 +122,25 @@ struct TreeAttnPlan {
   size_t ws_bytes;   // partials of the splits
 };
 
-// Above 32 columns, narrow tiles read a block once for every 32 columns, wide ones once for up to 256 but then all
-// wavefronts of a workgroup wait for each other at every block.  While the blocks of all groups fit the 256 MB
-// last-level cache the narrow ones win, beyond it the wide ones.  Measured (us), 32 columns against the widest, at 32K
-// with 64 blocks per list: one list per node (about 150 blocks in all): 32 and 64 nodes of 32 groups of 4 heads 57 and
-// 62, 78 and 98; 24 and 32 nodes of 64 groups 102 and 85, 115 and 94; of 128 groups 217 and 165 (32 nodes); 64 nodes of
-// 16 groups of 16 heads 78 and 108.  One list for all: 16 nodes of 64 groups 32 and 35, of 128 groups 49 and 57 (64
-// nodes 144 and 114), of 256 groups 110 and 94.
+// Above 32 columns a narrow tile (32) reads the blocks that its own nodes list, in as many workgroups as there are tiles;
+// a wide one reads a block once for all its columns, but its wavefronts wait for each other at every block, also those
+// whose nodes do not list it.  Widths between 32 and the narrowest that holds all columns (at most 256) are nowhere more
+// than 4 % below the better of the two.  Measured (us), 32 columns against the widest; 32K, 64 blocks per list unless said.
+// One list for all nodes: every wavefront works on every block, and the wide form wins once the narrow tiles need a
+// second round of the 256 CUs.  16 nodes of 4 heads (2 tiles): 128 groups 52 and 58, 144 groups 90 and 83; 32 nodes (4):
+// 64 groups 38 and 50, 80 groups 70 and 58; 64 nodes (8): 32 groups 39 and 51, 48 groups 70 and 63, 128 groups 158 and
+// 130; 27 nodes of 8 heads (7): 64 groups 74 and 71; 8 nodes of 16 heads (4): 64 groups 38 and 50, 128 groups 84 and 77;
+// 64 nodes of 16 heads (32): 16 groups 72 and 69, 64 groups 276 and 199.
+// A list per node: the nodes of a tree list about 3 times a list's blocks between them.  Up to 128 columns the wide form
+// wins from about 200 MB on.  27 nodes of 4 heads: 24, 32, 40, 64 and 128 groups 50 and 54, 63 and 62, 83 and 75, 131
+// and 101, 250 and 187; 13 nodes: 24, 32 and 128 groups 36 and 37, 45 and 41, 168 and 126; 27 nodes of 2 heads, 32
+// groups 51 and 46; 8 nodes of 8 heads, 32 and 64 groups 37 and 39, 68 and 63.  With lists of 16 blocks, 27 nodes of 4
+// heads: 96, 128 and 256 groups 67 and 85, 79 and 87, 164 and 143; of 32: 48 and 64 groups 55 and 60, 73 and 71; of 160
+// at 64K: 8, 16 and 24 groups 37 and 49, 73 and 70, 121 and 96.  Beyond 128 columns too many wavefronts wait, and the
+// narrow form is as fast or faster: 64 nodes of 4 heads: 32, 48, 64 and 128 groups 82 and 109, 155 and 154, 177 and 184,
+// 347 and 341; 40 nodes: 48, 64, 96 and 256 groups 101 and 132, 180 and 159, 204 and 295, 534 and 567; 64 nodes of 8
+// heads, 64 groups 250 and 290; 64 nodes of 16 heads with 96 blocks at 64K: 8, 16 and 48 groups 60 and 95, 119 and 166,
+// 385 and 581.
 // With fewer workgroups than CUs the blocks are split over them: at least half a block per wavefront, or three blocks
 // per workgroup where the wavefronts share them (one each: 19 -> 24 us for 22 nodes of 3 groups of 4 heads, 55 blocks).
 // The second launch reads up to 8 splits at once: beyond 16 the finer split of lists that differ by node costs what it
@@ -139,13 +151,9 @@ inline TreeAttnPlan tree_attn_plan(int64_t groups, int32_t n, int32_t group_size
   const int cols = n * group_size;
   const int64_t most_blocks = (t_max + 63) / 64;
   auto at_most = [&](int64_t x) { return most_blocks < x ? most_blocks : x; };
-  const int64_t bytes = groups * at_most((int64_t)k_total * (one_list || n == 1 ? 1 : 2)) * (2 * 64 * 128 * 2);
-  if (cols <= 16)
-    p.width = 16;
-  else if (cols <= 32 || bytes < ((int64_t)256 << 20))
-    p.width = 32;
-  else
-    p.width = cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
+  const int64_t narrow_wgs = groups * ((cols + 31) / 32), bytes = groups * at_most(3 * (int64_t)k_total) * (2 * 64 * 128 * 2);
+  const bool share = one_list ? narrow_wgs > 256 : cols <= 128 && bytes >= ((int64_t)192 << 20);
+  p.width = cols <= 16 ? 16 : cols <= 32 || !share ? 32 : cols <= 64 ? 64 : cols <= 128 ? 128 : 256;
   const int64_t wgs = groups * ((cols + p.width - 1) / p.width), blocks = at_most(k_total);
   int64_t ns = 256 / wgs;
   int64_t most = p.width <= 32 ? (2 * blocks + 2 + 7) / 8 : (blocks + 1 + 2) / 3;

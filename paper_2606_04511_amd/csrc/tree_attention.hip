@@ -30,7 +30,7 @@
 // with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 100 us, of which 9 before the
 // first product, 3 after the last; each of the 48 blocks of a workgroup takes 1.8 us, three blocks' loads in flight.
 // 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 123 us, a block read from L2 once per two nodes
-// (256 columns per workgroup: 143, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 13
+// (256 columns per workgroup: 166, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 13
 // us and 4 for the merge of the splits, a chain of latencies.
 #include <math.h>
 

@@ -16,11 +16,12 @@ pytestmark = pytest.mark.gpu
 # ---- attention: the last block of the largest cache ------------------------------------------------------
 
 LAST = [
-    # nodes, group, entries per list, one list: 16 columns; 32; 64 of wavefronts that share the blocks (the split of the
-    # work goes by the entries that a list may hold, not by those it holds)
+    # nodes, group, entries per list, one list: 16 columns; 32; two tiles of 32; 64 and 128 of wavefronts that share the
+    # blocks (the split of the work goes by the entries that lists may hold, not by those they hold)
     (1, 4, 6, False),
     (8, 4, 6, False),
     (9, 4, 8192, True),
+    (9, 4, 8192, False),
     (17, 4, 8192, False),
 ]
 
@@ -61,8 +62,8 @@ def test_attn_last_block_of_the_largest_cache(dev, case):  # noqa: F811
 
 # ---- attention: NaN in what a node attends ------------------------------------------------------------------
 
-# nodes, group, kv heads, batch, entries per list, t: 16 and 32 columns with splits and without, and the forms whose
-# wavefronts share the blocks (lists that may hold many entries), with splits and without
+# nodes, group, kv heads, batch, entries per list, t: 16 and 32 columns with splits and without, the form whose wavefronts
+# share the blocks (lists that may hold many entries) with splits, tiles of 32 without splits, the shared form without
 SPREAD = [
     (5, 3, 1, 2, 6, 700),
     (7, 4, 2, 2, 8, 1500),
@@ -136,6 +137,48 @@ def test_attn_nan_reaches_those_that_attend_it(dev, case, what):  # noqa: F811
     assert torch.equal(seen.all(3), bad) and torch.equal(seen.any(3), bad)
     keep = ~bad.to(dev)
     assert torch.equal(got[keep].view(torch.int16), plain[keep].view(torch.int16))
+
+
+# ---- attention: one list, many columns -------------------------------------------------------------------------
+
+ONE_LIST = [
+    # nodes, group, kv heads, batch, t: 160 columns of 256 with splits; 1024 in four tiles with splits; 256 of 256 in
+    # more workgroups than CUs; 18 of 32 there; 33 of 64
+    (40, 4, 12, 5, 900),
+    (64, 16, 3, 3, 5000),
+    (64, 4, 64, 4, 300),
+    (9, 2, 128, 4, 300),
+    (11, 3, 64, 4, 300),
+]
+
+
+@pytest.mark.parametrize("case", range(len(ONE_LIST)))
+def test_attn_one_list_for_many_columns(dev, case):  # noqa: F811
+    n, G, H, B, t = ONE_LIST[case]
+    say("tree attention, one list", ONE_LIST[case])
+    gen, rng = torch.Generator(device=dev).manual_seed(case), random.Random(case)
+    k = 7
+    s = shape_of(B, H, G, k, t, n)
+    mk = lambda *size: torch.randn(*size, generator=gen, device=dev, dtype=torch.bfloat16)  # noqa: E731
+    q, kk, vv, kt, vt = mk(B, H * G, n, D), mk(B, H, s.t_cap, D), mk(B, H, s.t_cap, D), mk(B, H, n, D), mk(B, H, n, D)
+    t_ctx = [t - 70 * b for b in range(B)]
+    parent = trees(rng, B, n, "wide", pad=[(B - 1, n - 2, n)])
+    nb = -(-t // L)
+    sel = torch.full((B, H, 1, k), -1, dtype=torch.int16, device=dev)
+    some = min(nb, k)
+    sel[..., :some] = torch.rand(B, H, 1, nb, generator=gen, device=dev).topk(some, dim=3).indices.to(torch.int16)
+    cnt = torch.randint(0, some + 1, (B, H, 1), generator=gen, device=dev).to(torch.int16)
+    o = torch.full(q.shape, NAN, dtype=torch.bfloat16, device=dev)
+    ws = workspace(dev, sp.sparda_workspace_size(s, sp.SPARDA_OP_TREE_ATTN, n, t))
+    sp.sparda_tree_attn(s, q, n, torch.tensor(t_ctx, dtype=torch.int32, device=dev), t, parent.to(dev), kk, vv, kt, vt,
+                        1, sel, cnt, ref.SCALE, o, ws)
+    torch.cuda.synchronize()
+    assert not torch.isnan(o).any()
+    for h in {0, H // 2, H - 1}:
+        x = [y[:, h:h + 1].cpu() for y in (kk, vv, kt, vt, sel, cnt)]
+        want, w = ref.attn(q[:, h * G:(h + 1) * G].cpu(), *x[:4], t_ctx, parent, *x[4:], ref.SCALE)
+        off = (o[:, h * G:(h + 1) * G].cpu().double() - want).abs()
+        assert bool((off <= ref.attn_bar(want, w)).all())
 
 
 # ---- attention: weights that must cancel --------------------------------------------------------------------
