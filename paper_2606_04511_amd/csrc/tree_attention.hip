@@ -51,7 +51,8 @@ constexpr int kTaBuf = kTaHalf * kHeadDim * 2;       // bytes of a half's K or V
 constexpr int kTaSlot = 4 * kTaBuf;                  // bytes of a block's K, then its V
 constexpr int kTaRing = 4;                           // blocks in LDS at once (shared form)
 constexpr int kTaWindow = 2048;                      // blocks per window of the table
-constexpr int kTaTree = -1;                          // the list's entry of the drafted tokens: no block has this number
+constexpr int kTaTree = 0x7fff;                      // the list's entry of the drafted tokens (others: 0 .. 2047)
+constexpr int kTaTreeBlock = 0x10000;                // as a block's number, past every block's: from here on
 constexpr int kTaPitch = kHeadDim + 4;               // floats per merged row: 16 rows of 16 bytes touch every bank once
 constexpr int kTaPartial = kHeadDim + 4;             // floats of a split's partial: m, l, two unused, the sums
 constexpr int kCombineThreads = 256;
@@ -431,7 +432,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
   const uint32_t k_off = r4 * 256 + 16 * ((lane & 15) ^ r4), v_off = r4 * 256 + 16 * ((lane & 15) ^ (2 * r4));
   auto issue = [&](const uint16_t* cache, const uint16_t* drafted, int j, int hf, uint32_t off0, int flip, int by,
                    uint32_t dst) {
-    if (j != kTaTree) {
+    if (j < kTaTreeBlock) {
       const char* src = reinterpret_cast<const char*>(cache + (u.bm * a.t_cap + (int64_t)j * kBlock + hf * kTaHalf) * kHeadDim);
 #pragma unroll
       for (int i = 0; i < 8; ++i) lds_load16<kOnce>(src + 1024 * i, off0 ^ ((i & flip) << by), dst + 1024 * i);
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
     bool tree_here;
     const int n_list = lists.window(a, u, w0, nb, lds, &tree_here);
     const int n_items = 2 * n_list - (tree_here && n <= kTaHalf ? 1 : 0);
-    auto block_of = [&](int j) { return j == kTaTree ? j : j + w0; };
+    auto block_of = [&](int j) { return j + (j == kTaTree ? kTaTreeBlock : w0); };
     cols.chunk = -1;
     int x = wave;
     int j = 0;
@@ -464,7 +465,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_kernel(TreeAttnArgs a, i
     lds_loads_landed();  // the first half and the queries: from here on the loads are counted
     while (x < n_items) {
       const int e = x >> 1, hf = x & 1, x2 = x + kTaWaves;
-      const bool more = x2 < n_items, tree = j == kTaTree;
+      const bool more = x2 < n_items, tree = j >= kTaTreeBlock;
       if (e >> 6 != cols.chunk) cols.scan(a, lds, e, n_list);
       const int j2 = more ? block_of(cols.entry(lds, x2 >> 1)) : 0;
       const uint32_t valid = half_valid(u, tree, j, hf);
@@ -556,7 +557,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(lds.kv)) + wave * 2048;
   auto issue = [&](int j, int slot) {
     const uint32_t dst = ring_at + slot * kTaSlot;
-    const bool tree = j == kTaTree;
+    const bool tree = j >= kTaTreeBlock;
     const int64_t at = (tree ? u.bm * n : u.bm * a.t_cap + (int64_t)j * kBlock) * kHeadDim;
     const uint16_t* const kp = (tree ? a.kt : a.k) + at;
     const uint16_t* const vp = (tree ? a.vt : a.v) + at;
@@ -574,7 +575,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
   for (int w0 = 0; w0 == 0 || w0 < nb; w0 += kTaWindow) {
     bool tree_here;
     const int n_list = lists.window(a, u, w0, nb, lds, &tree_here);
-    auto block_of = [&](int j) { return j == kTaTree ? j : j + w0; };
+    auto block_of = [&](int j) { return j + (j == kTaTree ? kTaTreeBlock : w0); };
     cols.chunk = -1;
     lds_loads_landed();  // the queries: from here on the loads are counted, 4 per block
 #pragma unroll 1
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(kTaThreads) void tree_attn_shared_kernel(TreeAttnAr
     for (int s = 0; s < n_list; ++s) {
       if (s >> 6 != cols.chunk) cols.scan(a, lds, s, n_list);
       const int j = block_of(cols.entry(lds, s));
-      const bool tree = j == kTaTree;
+      const bool tree = j >= kTaTreeBlock;
       char* const kslot = lds.kv + (s % kTaRing) * kTaSlot;
       char* const vslot = kslot + 2 * kTaBuf;
       // this wavefront's rows of block s have landed (two more blocks may be under way), the rows of V that no column
