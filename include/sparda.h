@@ -123,8 +123,8 @@ enum sparda_op {
  *                 of Alg. 2: one window per L tokens on the (64, 64) grid, one per 16 on
  *                 (32, 16)); win_begin == win_end is a no-op.
  *   k_cmp   out : bf16 [B][Hkv][nc_cap][D] device; only rows [win_begin, win_end) are written.
- *   K~_i = round_to_nearest_even_bf16( (1/l_C) * sum of the l_C keys of window i ), the sum being
- *   exact for bf16 inputs (float64 accumulation), so the result does not depend on order.
+ *   K~_i = round_to_nearest_even_bf16( (1/l_C) * sum of the l_C keys of window i ), the sum taken in
+ *   float64: exact, whatever its order, for keys within 39 binades of each other.
  */
 int sparda_compress_keys(const sparda_shape* shape, const void* k_cache, int64_t t_ctx, int32_t win_begin,
                          int32_t win_end, void* k_cmp, hipStream_t stream);
@@ -430,11 +430,10 @@ int sparda_tree_select(const sparda_shape* shape, const void* f, int32_t n_nodes
  *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_TREE_ATTN).
  * o_i = softmax(sm_scale q_i K^T) V over the tokens t < t_ctx of node i's blocks and the tokens of
  * A(i): bf16 inputs, float32 accumulation and online softmax; a weight enters the product with V to
- * within 2^-16 of itself.  Whatever the caches hold from t_ctx
- * on, and whatever lies in the rows of absent nodes, has no effect.  The V of a block that any node
- * of a tree lists, and of its present nodes, has to be finite: a matrix product serves several nodes,
- * and those that do not attend a row meet it with weight 0.  A NaN in a node's query, or in a key
- * that it attends, makes its output NaN.
+ * within 2^-16 of itself.  Whatever the caches hold from t_ctx on, and whatever lies in the rows of
+ * absent nodes, has no effect.  The V of a block that any node of a tree lists, and of its present
+ * nodes, has to be finite: a matrix product serves several nodes, and those that do not attend a row
+ * meet it with weight 0.  A NaN in a node's query, or in a key that it attends, makes its output NaN.
  */
 int sparda_tree_attn(const sparda_shape* shape, const void* q, int32_t n_nodes, const int32_t* t_ctx, int64_t t_max,
                      const int32_t* parent, const void* k, const void* v, const void* k_tree, const void* v_tree,
@@ -468,7 +467,8 @@ enum sparda_prob_type { SPARDA_PROB_F32 = 0, SPARDA_PROB_BF16 = 1 };
  * is the first y at which the running sum of m exceeds u_0 sum m.  If the last rejection left no
  * weight at all it is undone for that draw; a rejection with q that leaves none is undone before
  * the next sibling is tested.  A probability that is not a positive finite number counts as 0.
- * Products, differences and sums are taken in float64.  Deterministic.
+ * Products, differences and sums are taken in float64.  Deterministic.  With q, each test of a sibling
+ * after a rejection reads the rows once more and replays the parent's earlier rejections.
  */
 int sparda_tree_verify(const sparda_shape* shape, int32_t n_nodes, int32_t vocab, int64_t ld, int32_t prob_type,
                        const void* p, const void* q, const int32_t* tokens, const int32_t* parent, const float* u,

@@ -5,8 +5,9 @@
 // One workgroup per (window i, batch*group row).  The window's l x 128 bf16 keys are one
 // contiguous run; 256 threads read it with 16-byte loads (thread t: dims 8*(t%16)..+7 of token
 // rows t/16 + 16 x), 1 KiB contiguous per wavefront load.  Partial sums are float64, so the sum
-// of at most 64 bf16 values is exact and the result does not depend on the reduction order; the
-// mean is rounded once to bf16.  HBM-bound: 2 l x 128 bytes read + 256 B written per window.
+// of at most 64 bf16 values within 39 binades of each other is exact and does not depend on the
+// reduction order (beyond that it does, and tree_commit.hip adds in the same order); the mean is
+// rounded once to bf16.  HBM-bound: 2 l x 128 bytes read + 256 B written per window.
 #include "device_util.hpp"
 #include "launch.hpp"
 

