@@ -20,8 +20,8 @@
 //      score exceeds it by more than 2^8; O^T += V^T P^T on the same MFMA, V read through the transposing
 //      LDS read.  P enters the product as two bf16 numbers, itself rounded and what that rounding took, so
 //      a weight is off by at most 2^-16 of itself; the denominators sum it in float32.  With the rounded
-//      one alone (2^-8) the products take half the instructions (27 nodes of 64 groups below: 89 us instead
-//      of 99; 16 nodes of 256 groups 90.5 and 92), but a step over a tree would be less exact than the
+//      one alone (2^-8) the products take half the instructions (27 nodes of 64 groups below: 88 us instead
+//      of 99; 16 nodes of 256 groups 90 and 92-95), but a step over a tree would be less exact than the
 //      decode steps it stands for.
 //   4. The wavefronts' states merge through LDS; with splits their float32 partials go to the workspace
 //      and a second launch merges them.
