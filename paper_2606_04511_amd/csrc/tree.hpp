@@ -137,7 +137,7 @@ struct TreeAttnPlan {
 // groups 51 and 46; 8 nodes of 8 heads, 32 and 64 groups 37 and 39, 68 and 63.  With lists of 16 blocks, 27 nodes of 4
 // heads: 96, 128 and 256 groups 67 and 85, 79 and 87, 164 and 143; of 32: 48 and 64 groups 55 and 60, 73 and 71; of 160
 // at 64K: 8, 16 and 24 groups 37 and 49, 73 and 70, 121 and 96.  Beyond 128 columns too many wavefronts wait, and the
-// narrow form is as fast or faster: 64 nodes of 4 heads: 32, 48, 64 and 128 groups 82 and 109, 155 and 154, 177 and 184,
+// narrow form is within 13 % or faster, often by much: 64 nodes of 4 heads: 32, 48, 64 and 128 groups 82 and 109, 155 and 154, 177 and 184,
 // 347 and 341; 40 nodes: 48, 64, 96 and 256 groups 101 and 132, 180 and 159, 204 and 295, 534 and 567; 64 nodes of 8
 // heads, 64 groups 250 and 290; 64 nodes of 16 heads with 96 blocks at 64K: 8, 16 and 48 groups 60 and 95, 119 and 166,
 // 385 and 581.
