@@ -37,6 +37,13 @@
  *   sparda_tree_verify      probabilities, random numbers -> the accepted path and the next token
  *   sparda_tree_commit      the accepted path's K and V -> the caches of all layers, and K~
  *
+ * and, for serving sequences of different lengths whose tokens lie in pages:
+ *
+ *   sparda_rotate           rotary positions of query, key or Forecast rows, or the gradient through them
+ *   sparda_paged_append     new tokens' K (rotated on the way) and V -> the pages, and K~; their Q and F rotated
+ *   sparda_paged_select     F, paged K~ -> the block set of every sequence's newest token
+ *   sparda_paged_attn       Q, paged K and V -> O: its listed blocks, or its whole context
+ *
  * Conventions shared by every call:
  *   - Every function returns an int status: SPARDA_OK (0) or a negative SPARDA_ERR_* code.  No
  *     call throws, aborts or prints.  sparda_last_error_detail() gives a human-readable reason
@@ -109,7 +116,9 @@ enum sparda_op {
   SPARDA_OP_INDEXER_KL = 4,
   SPARDA_OP_DECODE_STEP = 5,
   SPARDA_OP_TREE_SELECT = 6, /* n_q = n_nodes, q_pos0 = t_max */
-  SPARDA_OP_TREE_ATTN = 7    /* n_q = n_nodes, q_pos0 = t_max */
+  SPARDA_OP_TREE_ATTN = 7,   /* n_q = n_nodes, q_pos0 = t_max */
+  SPARDA_OP_PAGED_SELECT = 16, /* n_q = 1, q_pos0 = t_max - 1 */
+  SPARDA_OP_PAGED_ATTN = 17   /* n_q = 1, q_pos0 = t_max - 1 */
 };
 
 /*
@@ -497,6 +506,171 @@ int sparda_tree_commit(const sparda_shape* shape, int32_t n_nodes, const int32_t
                        const int32_t* n_path, int32_t n_layers, const void* const* k_tree, const void* const* v_tree,
                        void* const* k_cache, void* const* v_cache, void* const* k_cmp, int32_t* t_new,
                        hipStream_t stream);
+
+/*
+ * ---- Paged caches ------------------------------------------------------------------------------
+ *
+ * A server's sequences differ in length and grow.  Their K, V and K~ lie in pages of P tokens, taken from
+ * pools in any order; a table names the pages of each sequence.  Rotary positions turn a key before it is
+ * cached (and so before it is compressed), and the queries and Forecast rows that meet it.
+ *   t_ctx   in : int32 [B] device, tokens of each sequence; zero or less: an absent sequence (for the
+ *                append a negative value only: it may begin a sequence).
+ *   t_max      : no t_ctx is larger (one that is counts as t_max); it sizes workspaces and grids;
+ *                1 <= t_max <= t_cap.
+ *   shape      : t_cap bounds the tokens of a sequence; nc_cap is not used.
+ * Lengths and tables are read on the device: all calls may be captured into a graph.
+ */
+
+/* Strided rows of D elements: row (b, head, token) begins at data + b ld_batch + head ld_head + token
+ * ld_token elements.  data is 16-byte aligned and every stride a multiple of 16 bytes, in [0, 2^40).  The
+ * stride of a dimension of size 1 is not used.  A stride of 0 repeats rows (inputs only); the rows of an
+ * output must not overlap: sorted, each stride has to clear what the smaller ones span. */
+typedef struct sparda_rows {
+  void* data;
+  int64_t ld_batch, ld_head, ld_token;
+} sparda_rows;
+
+enum sparda_type { SPARDA_F32 = 0, SPARDA_BF16 = 1 };
+
+/* Which elements of a head form pair j < rot_dim / 2. */
+enum sparda_rope_layout {
+  SPARDA_ROPE_HALF = 0, /* (j, j + rot_dim / 2) */
+  SPARDA_ROPE_PAIRS = 1 /* (2 j, 2 j + 1)       */
+};
+
+/* Rotary positions: pair j of a row at position p turns by the angle p freq[j]. */
+typedef struct sparda_rope {
+  uint32_t struct_size; /* = sizeof(sparda_rope)                                                     */
+  int32_t rot_dim;      /* the head's first rot_dim elements turn, the others pass; 0, 16, 32 .. 128 */
+  int32_t layout;       /* a sparda_rope_layout                                                      */
+  float scale;          /* factor on the turned elements (normally 1; scaled contexts raise it)      */
+  const double* freq;   /* device float64 [rot_dim / 2], radians per position (not read if rot_dim 0) */
+} sparda_rope;
+
+/* Scalings of the frequencies for contexts longer than the trained one. */
+enum sparda_rope_scaling {
+  SPARDA_ROPE_PLAIN = 0,   /* base^(-2 j / rot_dim)                                                    */
+  SPARDA_ROPE_LINEAR = 1,  /* divided by factor: positions are interpolated                            */
+  SPARDA_ROPE_BASE = 2,    /* base times factor^(rot_dim / (rot_dim - 2)): the slowest pair is divided
+                              by factor, the fastest kept                                              */
+  SPARDA_ROPE_BANDS = 3,   /* by the turns that a pair makes over the trained context: pairs with less
+                              than `low` are divided by factor, with more than `high` kept, between
+                              them blended linearly in the turns; scale 1 + 0.1 ln factor              */
+  SPARDA_ROPE_FACTORS = 4  /* pair j divided by factors[j] (searched factors, as the paper's models use,
+                              App. C); scale sqrt(1 + ln factor / ln t_train)                          */
+};
+
+/*
+ * sparda_rope_freqs -- the frequency table of a rotation, on the host (no GPU work): freq[j] for
+ * j < rot_dim / 2 in float64, and the scale that goes with it (1 where none is named above).
+ *   rot_dim    : 16, 32 .. 128.
+ *   base       : finite, > 1.
+ *   factor     : how much longer the context is, finite, >= 1 (not read by PLAIN).
+ *   t_train    : tokens of the trained context, > 1 (BANDS and FACTORS).
+ *   low, high  : 0 <= low < high, finite (BANDS).
+ *   factors    : host float64 [rot_dim / 2], finite and > 0 (FACTORS).
+ *   freq   out : host float64 [rot_dim / 2]; the caller copies it to the device.
+ *   scale  out : host float.
+ */
+int sparda_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, double t_train, double low,
+                      double high, const double* factors, double* freq, float* scale);
+
+/*
+ * sparda_rotate -- rotary positions of rows, or the gradient through them.
+ *   type       : the elements of x and y, a sparda_type.
+ *   batch, n_heads, n_tok : rows; any of them 0 is a no-op; batch n_tok <= 2^28.
+ *   x      in  : rows [batch][n_heads][n_tok][D].
+ *   pos    in  : int32 device, token t of sequence b at pos[b pos_ld + t]; any value.  pos_ld 0: one
+ *                row of positions for all sequences, else pos_ld >= n_tok.
+ *   y      out : rows, the same sizes; x itself (in place, with the same strides), or memory that does
+ *                not overlap it.
+ *   backward   : 0, or 1: the transposed rotation, which takes the gradient with respect to y to the
+ *                one with respect to x (sparda_indexer_kl's d_f, say).
+ * With (a, b) pair j of a row at position p and w = p freq[j]:
+ *   y_a = scale (x_a cos w - x_b sin w), y_b = scale (x_a sin w + x_b cos w);
+ * backward: w negated.  The angle is reduced in float64, products in float32, one rounding.
+ */
+int sparda_rotate(const sparda_rope* rope, int32_t type, int32_t batch, int32_t n_heads, int64_t n_tok,
+                  const sparda_rows* x, const int32_t* pos, int64_t pos_ld, const sparda_rows* y, int32_t backward,
+                  hipStream_t stream);
+
+/* The pages of one layer.  Token t of sequence b lies in page table[b table_ld + t / P], row t % P.  An entry
+ * outside [0, n_pages) is no page: tokens there are neither stored nor attended, their windows have no key. */
+typedef struct sparda_pages {
+  uint32_t struct_size; /* = sizeof(sparda_pages)                                                     */
+  int32_t page_size;    /* P: 16, 32, 64 .. 65536 tokens                                              */
+  int64_t n_pages;      /* pages in the pools, 1 .. 2^31 - 1                                          */
+  int64_t table_ld;     /* entries from one sequence's row to the next; table_ld P >= t_cap           */
+  int64_t page_ld;      /* elements from one page of k, and of v, to the next: a multiple of 8,
+                           >= Hkv P D, < 2^40                                                         */
+  const int32_t* table; /* device                                                                     */
+  void* k;              /* device bf16 [n_pages][Hkv][P][D], pages page_ld apart                      */
+  void* v;              /* the same                                                                   */
+  void* k_cmp;          /* device bf16 [n_pages][Hkv][P / s_C][D]: window i with the page of its first
+                           token, i s_C; P has to be a multiple of s_C                                */
+} sparda_pages;
+
+/*
+ * sparda_paged_append -- new tokens into a layer's pages (the append of Alg. 2, for sequences of different
+ * lengths), the compressed keys of the windows that they complete (Sec. 3, Eq. 2), and the tokens' queries
+ * and Forecast rows turned to the same positions.
+ *   pages      : k, v; k_cmp may be NULL: no compressed keys.
+ *   rope       : NULL: nothing turns.
+ *   n_max      : tokens per sequence in the rows below, 1 .. t_cap; B Hkv n_max <= 2^27.
+ *   n_new  in  : int32 [B] device, tokens that sequence b really has (clamped to 0 .. n_max); NULL: n_max.
+ *   t_ctx  in  : int32 [B] device, tokens before the call; new token j is at position t_ctx + j.  Tokens
+ *                that would lie past t_cap are dropped.
+ *   k_new, v_new in : bf16 rows [B][Hkv][n_max][D].
+ *   q, q_out   : bf16 rows [B][Hq][n_max][D]: the queries, and where they go turned; in place is allowed.
+ *                Both or neither NULL.
+ *   f, f_out   : bf16 rows [B][Hkv][n_max][D]: the same for the Forecast rows.
+ *   t_new  out : int32 [B] device: t_ctx plus the tokens taken (t_ctx itself for an absent sequence); not
+ *                the array t_ctx.
+ * K is rounded to bf16 once, after the rotation; the means are those of the rounded keys, with the bits of
+ * sparda_compress_keys; a window is written when it ends in (t_ctx, t_new] and all its tokens have pages.
+ * Rows of q_out and f_out past a sequence's tokens, and whatever else the pages hold, are left as they were.
+ * No page that receives a token may belong to two sequences; the buffers must not overlap.
+ */
+int sparda_paged_append(const sparda_shape* shape, const sparda_pages* pages, const sparda_rope* rope, int32_t n_max,
+                        const int32_t* n_new, const int32_t* t_ctx, const sparda_rows* k_new, const sparda_rows* v_new,
+                        const sparda_rows* q, const sparda_rows* q_out, const sparda_rows* f, const sparda_rows* f_out,
+                        int32_t* t_new, hipStream_t stream);
+
+/*
+ * sparda_paged_select -- the attended block set of every sequence's newest token (Sec. 4.1, Eq. 4; Eq. 1), as
+ * sparda_forecast_select gives it for a row at position t_ctx - 1.
+ *   pages      : k_cmp; k and v are not used.  Windows complete within t_ctx tokens that overlap a candidate
+ *                block are read; one without a page scores -inf.
+ *   f      in  : bf16 [B][Hkv][1][D] device.
+ *   t_ctx, t_max : as above, the new token among them.
+ *   sel, cnt out: int16 [B][Hkv][1][k_total] and [B][Hkv][1] device, as sparda_forecast_select writes them;
+ *                all -1 and 0 for an absent sequence.
+ *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_PAGED_SELECT).
+ */
+int sparda_paged_select(const sparda_shape* shape, const sparda_pages* pages, const void* f, const int32_t* t_ctx,
+                        int64_t t_max, int16_t* sel, int16_t* cnt, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * sparda_paged_attn -- attention of every sequence's newest token (Sec. 4.1, Eq. 5).
+ *   pages      : k and v; k_cmp is not used.
+ *   q      in  : bf16 [B][Hq][1][D] device.
+ *   t_ctx, t_max : as above, the new token among them.
+ *   sel, cnt in: int16 [B][Hkv][1][k_total] and [B][Hkv][1] device; any order; entries that hold no token of
+ *                the context are skipped, a block listed twice is attended once.  Both NULL: the whole context
+ *                (k_total is not used).
+ *   sm_scale   : logit scale, finite; normally 1/sqrt(D).
+ *   o      out : bf16 [B][Hq][1][D] device; zeros for a row that attends no token.
+ *   ws, ws_bytes: device workspace of at least sparda_workspace_size(SPARDA_OP_PAGED_ATTN); its size does
+ *                not depend on the lengths beyond t_max.
+ * o = softmax(sm_scale q K^T) V over the tokens t < t_ctx of the listed blocks, or all of them: bf16 inputs,
+ * float32 accumulation and online softmax; a weight enters the product with V to within 2^-16 of itself.
+ * Whatever the pages hold from t_ctx on has no effect.  A NaN in a query, or in a key or value that it attends, makes
+ * what depends on it NaN; an infinite value that is attended makes its element of the output infinite or NaN.
+ * Deterministic.
+ */
+int sparda_paged_attn(const sparda_shape* shape, const sparda_pages* pages, const void* q, const int32_t* t_ctx,
+                      int64_t t_max, const int16_t* sel, const int16_t* cnt, float sm_scale, void* o, void* ws,
+                      size_t ws_bytes, hipStream_t stream);
 
 /*
  * sparda_workspace_size -- device workspace bytes that call `op` (a sparda_op) needs for n_q

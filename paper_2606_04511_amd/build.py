@@ -24,7 +24,8 @@ PEAKS_SOURCE = "peaks.hip"
 PEAKS_LIB = os.path.join(PKG, "libsparda_peaks.so")
 
 SOURCES = ["compress.hip", "select.hip", "select_prefill.hip", "score_max.hip", "select_multihead.hip", "indexer_kl.hip", "attention.hip", "attention_prefill.hip", "gather.hip", "sparda_abi.cpp",
-           "tree_select.hip", "tree_attention.hip", "tree_verify.hip", "tree_commit.hip", "tree_abi.cpp"]
+           "tree_select.hip", "tree_attention.hip", "tree_verify.hip", "tree_commit.hip", "tree_abi.cpp",
+           "rotate.hip", "paged_append.hip", "paged_select.hip", "paged_attention.hip", "paged_abi.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
           "-Wall", "-Wno-unused-function"]

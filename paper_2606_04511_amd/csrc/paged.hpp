@@ -1,0 +1,155 @@
+// paged.hpp -- launchers, sizes and device helpers of the rotary positions and the operators over paged
+// caches (rotate.hip, paged_append.hip, paged_select.hip, paged_attention.hip; private to the library).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "launch.hpp"
+
+namespace sparda {
+
+struct Rows {  // strided rows of 128 elements (strides in elements)
+  void* data;
+  int64_t ld_batch, ld_head, ld_token;
+};
+
+struct Rope {
+  const double* freq;
+  int32_t rot_dim;  // 0: nothing turns
+  int32_t pairs;    // pair j is (2 j, 2 j + 1), else (j, j + rot_dim / 2)
+  float scale;
+};
+
+struct RotateArgs {
+  Rope rope;
+  Rows x, y;
+  const int32_t* pos;
+  int64_t pos_ld;
+  int32_t batch, n_heads;
+  int64_t n_tok;
+  int32_t bf16, backward;
+};
+
+// Where the tokens of a call's sequences lie.
+struct Pages {
+  const int32_t* table;
+  int64_t table_ld, page_ld;
+  int32_t n_pages;
+  int32_t shift;  // a page holds 2^shift tokens
+  uint16_t* k;
+  uint16_t* v;
+  uint16_t* kc;
+};
+
+struct PagedAppendArgs {
+  Pages pg;
+  Rope rope;
+  Rows k_new, v_new, q, q_out, f, f_out;  // data null: absent
+  const int32_t* n_new;                   // null: n_max
+  const int32_t* t_ctx;
+  int32_t* t_new;
+  int32_t batch, n_kv_heads, group_size, n_max;
+  int64_t t_cap;
+  WinGrid grid;
+};
+
+struct PagedSelectArgs {
+  Pages pg;
+  const uint16_t* f;
+  const int32_t* t_ctx;
+  int64_t t_max;
+  int16_t* sel;
+  int16_t* cnt;
+  float* ws;           // block scores: row stride ws_stride, the first candidate at slot 0
+  int64_t ws_stride;
+  int32_t batch, n_kv_heads, n_init, n_local, k_total;
+  WinGrid grid;
+};
+
+struct PagedAttnArgs {
+  Pages pg;
+  const uint16_t* q;
+  const int32_t* t_ctx;
+  int64_t t_max;
+  const int16_t* sel;  // null: whole contexts
+  const int16_t* cnt;
+  uint16_t* o;
+  float* ws;
+  int32_t batch, n_kv_heads, group_size, k_total;
+  float scale_log2;
+};
+
+inline int64_t paged_select_stride(int64_t t_max, int32_t n_init, int32_t n_local) {
+  const int64_t c = (t_max - 1) / 64 - n_local - n_init + 1;
+  return c > 0 ? (c + 3) & ~(int64_t)3 : 0;
+}
+inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32_t n_local) {
+  return (size_t)rows * (size_t)paged_select_stride(t_max, n_init, n_local) * sizeof(float);
+}
+
+// How an attention call is cut.  Its work is a line of units of 32 tokens, row by row; every wavefront takes an equal
+// piece of the line, whatever the lengths are, and a piece that holds only a part of a row leaves a partial result.
+constexpr int kPagedWaves = 8;    // wavefronts of a workgroup
+constexpr int kPagedMaxWgs = 256; // one workgroup per CU
+struct PagedPlan {
+  int32_t n_wgs;
+  int64_t row_units;  // units of a row (sparse calls; dense ones follow the lengths)
+  bool joined;        // rows may be cut between workgroups, or shared by wavefronts of one that holds other rows
+};
+inline PagedPlan paged_attn_plan(int64_t rows, int64_t t_max, int32_t k_total, bool sparse) {
+  PagedPlan p;
+  if (sparse) {
+    // up to one row per CU: workgroups per row; a row's units are rounded up to fill their wavefronts evenly (those
+    // past k_total are empty)
+    const int64_t units = 2 * (int64_t)k_total;
+    if (rows <= kPagedMaxWgs) {
+      int64_t s = kPagedMaxWgs / rows;
+      const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
+      s = s < most ? s : most;
+      p.n_wgs = (int32_t)(rows * s);
+      p.row_units = (units + kPagedWaves * s - 1) / (kPagedWaves * s) * (kPagedWaves * s);
+      p.joined = s > 1;
+    } else {
+      p.n_wgs = kPagedMaxWgs;
+      p.row_units = units;
+      p.joined = true;
+    }
+  } else {
+    const int64_t most = (rows * ((t_max + 31) / 32) + kPagedWaves - 1) / kPagedWaves;
+    p.n_wgs = (int32_t)(most < kPagedMaxWgs ? most : kPagedMaxWgs);
+    p.row_units = 0;
+    p.joined = true;
+  }
+  return p;
+}
+// Two partial results per wavefront, each per head: 128 sums, the maximum and the denominator (4 floats apart).
+constexpr int kPartFloats = 132;
+inline size_t paged_attn_ws(int32_t group_size) {
+  return (size_t)kPagedMaxWgs * kPagedWaves * 2 * (size_t)group_size * kPartFloats * sizeof(float);
+}
+
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t stream);
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
+hipError_t launch_paged_select(const PagedSelectArgs& a, hipStream_t stream);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t stream);
+
+// ---- device helpers ------------------------------------------------------------------------------
+
+// The page that holds token `tok` of the sequence whose table row is `row`; -1: none.
+__device__ __forceinline__ int32_t page_of(const Pages& pg, const int32_t* row, int64_t tok) {
+  const int32_t p = row[tok >> pg.shift];
+  return (uint32_t)p < (uint32_t)pg.n_pages ? p : -1;
+}
+// First element of token `tok` of KV head h in page p, of k and of v.
+__device__ __forceinline__ int64_t token_at(const Pages& pg, int32_t p, int h, int64_t tok) {
+  return p * pg.page_ld + (((int64_t)h << pg.shift) + (tok & (((int64_t)1 << pg.shift) - 1))) * 128;
+}
+// First element of the compressed key of the window that begins at token `tok`.
+__device__ __forceinline__ int64_t key_at(const Pages& pg, int32_t p, int n_kv_heads, int h, int64_t tok, int stride_log2) {
+  const int64_t slot = (tok & (((int64_t)1 << pg.shift) - 1)) >> stride_log2;
+  return ((((int64_t)p * n_kv_heads + h) << (pg.shift - stride_log2)) + slot) * 128;
+}
+
+}  // namespace sparda

@@ -12,6 +12,7 @@
 
 #include "abi_checks.hpp"
 #include "launch.hpp"
+#include "paged.hpp"
 #include "tree.hpp"
 
 using namespace sparda::abi;
@@ -261,6 +262,11 @@ int sparda_workspace_size(const sparda_shape* shape, int32_t op, int32_t n_q, in
       *bytes = sparda::tree_select_ws(groups, q_pos0, n_q, shape->n_init, shape->n_local);
     else
       *bytes = sparda::tree_attn_ws(groups, n_q, shape->group_size, shape->k_total, q_pos0);
+  } else if (op == SPARDA_OP_PAGED_SELECT || op == SPARDA_OP_PAGED_ATTN) {
+    if (n_q != 1) return fail(SPARDA_ERR_INVALID_ARG, "a paged call has n_q == 1");
+    const int64_t rows = (int64_t)shape->batch * shape->n_kv_heads;
+    *bytes = op == SPARDA_OP_PAGED_SELECT ? sparda::paged_select_ws(rows, q_pos0 + 1, shape->n_init, shape->n_local)
+                                          : sparda::paged_attn_ws(shape->group_size);
   } else {
     return fail(SPARDA_ERR_INVALID_ARG, "unknown op %d", op);
   }

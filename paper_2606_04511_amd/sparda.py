@@ -29,14 +29,26 @@ SPARDA_OP_INDEXER_KL = 4
 SPARDA_OP_DECODE_STEP = 5
 SPARDA_OP_TREE_SELECT = 6
 SPARDA_OP_TREE_ATTN = 7
+SPARDA_OP_PAGED_SELECT = 16
+SPARDA_OP_PAGED_ATTN = 17
 SPARDA_PROB_F32 = 0
 SPARDA_PROB_BF16 = 1
+SPARDA_F32 = 0
+SPARDA_BF16 = 1
+SPARDA_ROPE_HALF = 0
+SPARDA_ROPE_PAIRS = 1
+SPARDA_ROPE_PLAIN = 0
+SPARDA_ROPE_LINEAR = 1
+SPARDA_ROPE_BASE = 2
+SPARDA_ROPE_BANDS = 3
+SPARDA_ROPE_FACTORS = 4
 SPARDA_NOALLOC_SCRATCH_BYTES = 4718592  # the static scratch of sparda_sparse_attn_noalloc (include/sparda.h)
 
 EXPORTED = ("sparda_compress_keys", "sparda_forecast_select", "sparda_forecast_score_max", "sparda_multihead_select",
             "sparda_sparse_attn", "sparda_sparse_attn_noalloc", "sparda_gather_blocks", "sparda_stage_append_kv", "sparda_writeback_kv", "sparda_plan_staging", "sparda_indexer_kl",
             "sparda_tree_select", "sparda_tree_attn", "sparda_tree_verify", "sparda_tree_verify_workspace_size",
-            "sparda_tree_commit", "sparda_workspace_size", "sparda_status_string", "sparda_last_error_detail")
+            "sparda_tree_commit", "sparda_rope_freqs", "sparda_rotate", "sparda_paged_append", "sparda_paged_select",
+            "sparda_paged_attn", "sparda_workspace_size", "sparda_status_string", "sparda_last_error_detail")
 
 
 class _CShape(ctypes.Structure):
@@ -73,6 +85,55 @@ class SpardaShape:
         return _CShape(ctypes.sizeof(_CShape), self.batch, self.n_kv_heads, self.group_size, self.head_dim,
                        self.block_size, self.cmp_kernel, self.cmp_stride, self.n_init, self.n_local, self.k_total,
                        self.t_cap, self.nc_cap)
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld_batch", ctypes.c_int64), ("ld_head", ctypes.c_int64),
+                ("ld_token", ctypes.c_int64)]
+
+
+class _CRope(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+
+class _CPages(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+                ("table_ld", ctypes.c_int64), ("page_ld", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_cmp", ctypes.c_void_p)]
+
+
+class SpardaRope:
+    """A rotation (struct sparda_rope), made once for a model.  freq: float64 tensor on the GPU, radians per position."""
+
+    def __init__(self, rot_dim: int, layout: int, freq, scale: float = 1.0):
+        _expect(freq, "freq", torch.float64, rot_dim // 2)
+        self.freq = freq
+        self.c = _CRope(ctypes.sizeof(_CRope), rot_dim, layout, scale, _p(freq))
+
+
+class SpardaPages:
+    """The pages of one layer (struct sparda_pages), made once: it holds the tensors and their addresses.
+    table: int32 [B][pages of a sequence]; k, v: bf16 [n_pages][Hkv][P][128] (views of one pool with the same stride
+    between pages are fine); k_cmp: bf16 [n_pages][Hkv][P / stride][128], dense.  What a call does not use can be None."""
+
+    def __init__(self, page_size: int, table, k=None, v=None, k_cmp=None):
+        pools = [x for x in (k, v, k_cmp) if x is not None]
+        if not pools or len({x.shape[0] for x in pools}) != 1:
+            raise ValueError("k, v and k_cmp have the same number of pages")
+        for x, name in ((k, "k"), (v, "v"), (k_cmp, "k_cmp")):
+            if x is not None and (x.dtype != torch.bfloat16 or x.dim() != 4 or not x[0].is_contiguous()):
+                raise ValueError(f"{name}: bf16 [n_pages][Hkv][tokens][128] with dense pages")
+        if (k is None) != (v is None) or (k is not None and k.stride(0) != v.stride(0)):
+            raise ValueError("k and v come together, with one stride between pages")
+        if k_cmp is not None and not k_cmp.is_contiguous():
+            raise ValueError("k_cmp is not dense")
+        if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1:
+            raise ValueError("table: int32 [B][pages of a sequence]")
+        self.tensors = (table, k, v, k_cmp)
+        self.c = _CPages(ctypes.sizeof(_CPages), page_size, pools[0].shape[0],
+                         table.stride(0) if table.shape[0] > 1 else table.shape[1], 0 if k is None else k.stride(0),
+                         _p(table), _p(k), _p(v), _p(k_cmp))
 
 
 class SpardaError(RuntimeError):
@@ -116,7 +177,15 @@ def load() -> ctypes.CDLL:
         lib.sparda_tree_verify.argtypes = [S, i32, i32, i64, i32, P, P, P, P, P, P, P, P, P, sz, P]
         lib.sparda_tree_verify_workspace_size.argtypes = [S, i32, i32, ctypes.POINTER(sz)]
         lib.sparda_tree_commit.argtypes = [S, i32, P, P, P, i32, P, P, P, P, P, P, P]
-        for name in ("sparda_tree_select", "sparda_tree_attn", "sparda_tree_verify",
+        R, W, G = ctypes.POINTER(_CRope), ctypes.POINTER(_CRows), ctypes.POINTER(_CPages)
+        f64 = ctypes.c_double
+        lib.sparda_rope_freqs.argtypes = [i32, f64, i32, f64, f64, f64, f64, P, P, ctypes.POINTER(ctypes.c_float)]
+        lib.sparda_rotate.argtypes = [R, i32, i32, i32, i64, W, P, i64, W, i32, P]
+        lib.sparda_paged_append.argtypes = [S, G, R, i32, P, P, W, W, W, W, W, W, P, P]
+        lib.sparda_paged_select.argtypes = [S, G, P, P, i64, P, P, P, sz, P]
+        lib.sparda_paged_attn.argtypes = [S, G, P, P, i64, P, P, ctypes.c_float, P, P, sz, P]
+        for name in ("sparda_rope_freqs", "sparda_rotate", "sparda_paged_append", "sparda_paged_select",
+                     "sparda_paged_attn", "sparda_tree_select", "sparda_tree_attn", "sparda_tree_verify",
                      "sparda_tree_verify_workspace_size", "sparda_tree_commit",
                      "sparda_compress_keys", "sparda_forecast_select", "sparda_forecast_score_max",
                      "sparda_multihead_select", "sparda_sparse_attn", "sparda_sparse_attn_noalloc", "sparda_decode_step",
@@ -152,6 +221,33 @@ def _p(x):
     if isinstance(x, int):
         return x
     return x.data_ptr()
+
+
+def _expect(x, name: str, dtype, numel: int):
+    """A dense tensor of `numel` elements at least (ints and None pass: raw addresses)."""
+    if x is None or isinstance(x, int):
+        return
+    if x.dtype != dtype or not x.is_contiguous() or x.numel() < numel:
+        raise ValueError(f"{name}: {numel} dense elements of {dtype} expected")
+
+
+def _here(*tensors):
+    """The tensors are in the memory of the current device, whose stream the call goes to."""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2  # (-1: a tensor in host memory)
+    for x in tensors:
+        if x is not None and not isinstance(x, (int, tuple)) and x.get_device() != dev:
+            raise ValueError(f"a tensor is on {x.device}, the current device is {'cuda:%d' % dev if dev >= 0 else 'not in use'}")
+
+
+def _rows(x, name: str, shape, dtype=None):
+    """struct sparda_rows of a tensor [B][heads][tokens][128] of any strides, or of (address, ld_batch, ld_head, ld_token)."""
+    if x is None:
+        return None
+    if isinstance(x, tuple):
+        return ctypes.byref(_CRows(*x))
+    if x.shape != shape or (dtype is not None and x.dtype != dtype) or x.stride(3) != 1:
+        raise ValueError(f"{name}: {tuple(shape)} of {dtype} expected, its last dimension dense")
+    return ctypes.byref(_CRows(x.data_ptr(), x.stride(0), x.stride(1), x.stride(2)))
 
 
 # The current stream's handle without a Stream object around it (0.4 us instead of 2.9 us per call).
@@ -327,3 +423,55 @@ def sparda_tree_commit(shape: SpardaShape, n_nodes: int, t_ctx, path, n_path, n_
                                      _table(k_tree, n_layers), _table(v_tree, n_layers), _table(k_cache, n_layers),
                                      _table(v_cache, n_layers), _table(k_cmp, n_layers), _p(t_new), _stream(stream)),
            "sparda_tree_commit")
+
+
+def sparda_rope_freqs(rot_dim: int, base: float, scaling: int = SPARDA_ROPE_PLAIN, factor: float = 1.0, t_train: float = 0.0,
+                      low: float = 1.0, high: float = 32.0, factors=None):
+    """(float64 CPU tensor [rot_dim / 2] of radians per position, scale)."""
+    freq = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    scale = ctypes.c_float(0.0)
+    if factors is not None:
+        factors = torch.as_tensor(factors, dtype=torch.float64).contiguous()
+        _expect(factors, "factors", torch.float64, rot_dim // 2)
+    _check(load().sparda_rope_freqs(rot_dim, base, scaling, factor, t_train, low, high, _p(factors), _p(freq),
+                                    ctypes.byref(scale)), "sparda_rope_freqs")
+    return freq, float(scale.value)
+
+
+def sparda_rotate(rope: SpardaRope, type: int, batch: int, n_heads: int, n_tok: int, x, pos, pos_ld: int, y,
+                  backward: bool = False, stream=None):
+    dtype, size = torch.float32 if type == SPARDA_F32 else torch.bfloat16, (batch, n_heads, n_tok, 128)
+    _here(rope.freq, x, y, pos)
+    _check(load().sparda_rotate(ctypes.byref(rope.c), type, batch, n_heads, n_tok, _rows(x, "x", size, dtype), _p(pos),
+                                pos_ld, _rows(y, "y", size, dtype), int(backward), _stream(stream)), "sparda_rotate")
+
+
+def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int, n_new, t_ctx, k_new, v_new, q, q_out, f,
+                        f_out, t_new, stream=None):
+    cs, b, h, bf = shape.c(), shape.batch, shape.n_kv_heads, torch.bfloat16
+    kv, hq = (b, h, n_max, 128), (b, shape.n_q_heads, n_max, 128)
+    _here(rope.freq if rope else None, pages.tensors[0], n_new, t_ctx, k_new, v_new, q, q_out, f, f_out, t_new)
+    _check(load().sparda_paged_append(ctypes.byref(cs), ctypes.byref(pages.c), ctypes.byref(rope.c) if rope else None, n_max,
+                                      _p(n_new), _p(t_ctx), _rows(k_new, "k_new", kv, bf), _rows(v_new, "v_new", kv, bf),
+                                      _rows(q, "q", hq, bf), _rows(q_out, "q_out", hq, bf), _rows(f, "f", kv, bf),
+                                      _rows(f_out, "f_out", kv, bf), _p(t_new), _stream(stream)), "sparda_paged_append")
+
+
+def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max: int, sel, cnt, ws=None, ws_bytes: int = 0,
+                        stream=None):
+    cs = shape.c()
+    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
+        ws_bytes = ws.numel() * ws.element_size()
+    _here(pages.tensors[0], f, t_ctx, sel, cnt, ws)
+    _check(load().sparda_paged_select(ctypes.byref(cs), ctypes.byref(pages.c), _p(f), _p(t_ctx), t_max, _p(sel), _p(cnt),
+                                      _p(ws), ws_bytes, _stream(stream)), "sparda_paged_select")
+
+
+def sparda_paged_attn(shape: SpardaShape, pages: SpardaPages, q, t_ctx, t_max: int, sel, cnt, sm_scale: float, o, ws=None,
+                      ws_bytes: int = 0, stream=None):
+    cs = shape.c()
+    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
+        ws_bytes = ws.numel() * ws.element_size()
+    _here(pages.tensors[0], q, t_ctx, sel, cnt, o, ws)
+    _check(load().sparda_paged_attn(ctypes.byref(cs), ctypes.byref(pages.c), _p(q), _p(t_ctx), t_max, _p(sel), _p(cnt),
+                                    float(sm_scale), _p(o), _p(ws), ws_bytes, _stream(stream)), "sparda_paged_attn")

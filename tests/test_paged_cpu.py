@@ -1,0 +1,252 @@
+"""Paged caches and rotary positions without a GPU: refusals of the entry points (nothing is launched), workspace sizes,
+the frequency tables, and checks of the float64 definitions that the GPU tests compare with."""
+import ctypes
+import math
+import os
+
+import pytest
+import torch
+
+import paged_reference as ref
+import paper_2606_04511_amd.sparda as sp
+
+FAKE = 0x7F0000000000  # aligned, never dereferenced: validation fails before any launch
+BAD, UNSUP, WS = sp.SPARDA_ERR_INVALID_ARG, sp.SPARDA_ERR_UNSUPPORTED, sp.SPARDA_ERR_WORKSPACE
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    if not os.path.exists(sp.library_path()):
+        from paper_2606_04511_amd import build
+        build.build()
+    return sp.load()
+
+
+def shape(**kw):
+    base = dict(batch=2, n_kv_heads=8, group_size=4, k_total=16, t_cap=8192, nc_cap=0)
+    base.update(kw)
+    return sp.SpardaShape(**base)
+
+
+class Raw:
+    """A handle whose struct a test fills itself."""
+
+    def __init__(self, c):
+        self.c, self.tensors, self.freq = c, (None,), None
+
+
+def pages(**kw):
+    base = dict(size=ctypes.sizeof(sp._CPages), page_size=64, n_pages=256, table_ld=128, page_ld=8 * 64 * 128, table=FAKE,
+                k=FAKE, v=FAKE, k_cmp=FAKE)
+    base.update(kw)
+    return Raw(sp._CPages(*base.values()))
+
+
+def rope(**kw):
+    base = dict(size=ctypes.sizeof(sp._CRope), rot_dim=128, layout=0, scale=1.0, freq=FAKE)
+    base.update(kw)
+    return Raw(sp._CRope(*base.values()))
+
+
+def rc_of(fn, *args):
+    with pytest.raises(sp.SpardaError) as ei:
+        fn(*args)
+    assert sp.last_error_detail() != ""
+    return ei.value.status
+
+
+def replaced(args, **at):
+    """args with the named positions replaced ("a3": position 3)."""
+    out = list(args)
+    for k, v in at.items():
+        out[int(k[1:])] = v
+    return out
+
+
+PAGES = ((dict(size=0), BAD), (dict(page_size=0), BAD), (dict(page_size=-64), BAD), (dict(page_size=8), UNSUP),
+         (dict(page_size=48), UNSUP), (dict(page_size=131072), UNSUP), (dict(n_pages=0), BAD), (dict(n_pages=1 << 31), BAD),
+         (dict(table=None), BAD), (dict(table=FAKE + 2), BAD), (dict(table_ld=127), BAD), (dict(table_ld=-1), BAD))
+ROPES = ((dict(size=1), BAD), (dict(rot_dim=-2), BAD), (dict(rot_dim=130), BAD), (dict(rot_dim=33), BAD),
+         (dict(rot_dim=40), UNSUP), (dict(layout=2), BAD), (dict(scale=NAN), BAD), (dict(scale=INF), BAD),
+         (dict(freq=None), BAD), (dict(freq=FAKE + 4), BAD))
+ROWS = (None, (None, 128, 128, 128), (FAKE + 8, 1 << 20, 1 << 12, 128), (FAKE, -128, 1 << 12, 128), (FAKE, 1 << 40, 1 << 12, 128),
+        (FAKE, 1 << 20, 1 << 12, 132))
+OVERLAP = ((FAKE, 0, 1 << 12, 128), (FAKE, 1 << 20, 0, 128), (FAKE, 1 << 20, 1 << 12, 64), (FAKE, 1 << 12, 1 << 12, 128))
+
+
+def test_rotate_refusals():
+    f, x = sp.sparda_rotate, (FAKE, 1 << 20, 1 << 12, 128)
+    good = [rope(), sp.SPARDA_BF16, 2, 8, 7, x, FAKE, 7, (FAKE * 2, 1 << 20, 1 << 12, 128), 0]
+    for kw, status in ROPES:
+        assert rc_of(f, *replaced(good, a0=rope(**kw))) == status, kw
+    for at, status in ((dict(a1=2), BAD), (dict(a2=-1), BAD), (dict(a3=-1), BAD), (dict(a4=-1), BAD), (dict(a4=1 << 28), UNSUP),
+                       (dict(a6=None), BAD), (dict(a6=FAKE + 2), BAD), (dict(a7=6), BAD), (dict(a7=-1), BAD), (dict(a9=2), BAD),
+                       (dict(a8=(FAKE, 1 << 20, 1 << 13, 128)), BAD)):  # in place with other strides
+        assert rc_of(f, *replaced(good, **at)) == status, at
+    for r in ROWS:
+        assert rc_of(f, *replaced(good, a5=r)) == BAD, r
+        assert rc_of(f, *replaced(good, a8=r)) == BAD, r
+    for r in OVERLAP:
+        assert rc_of(f, *replaced(good, a8=r)) == BAD, r
+    assert rc_of(f, *replaced(good, a1=sp.SPARDA_F32, a5=(FAKE, 1 << 20, 1 << 12, 130))) == BAD
+    for at in (dict(a2=0), dict(a3=0), dict(a4=0)):  # no rows: nothing to do, whatever the pointers
+        f(*replaced(good, a5=None, a6=None, a8=None, **at))
+
+
+def test_append_refusals():
+    f, s = sp.sparda_paged_append, shape()
+    kv, q, q2 = (FAKE, 1 << 20, 1 << 12, 128), (FAKE, 1 << 22, 1 << 12, 128), (FAKE * 2, 1 << 22, 1 << 12, 128)
+    good = [s, pages(), rope(), 5, FAKE, FAKE, kv, kv, q, q2, kv, q2, FAKE * 2]
+    for kw, status in PAGES + ((dict(k=None), BAD), (dict(v=None), BAD), (dict(k=FAKE + 8), BAD), (dict(k_cmp=FAKE + 8), BAD),
+                               (dict(page_ld=8 * 64 * 128 - 8), BAD), (dict(page_ld=8 * 64 * 128 + 4), BAD),
+                               (dict(page_ld=1 << 40), BAD), (dict(page_size=32, table_ld=256), UNSUP)):
+        assert rc_of(f, *replaced(good, a1=pages(**kw))) == status, kw
+    for kw, status in ROPES:
+        assert rc_of(f, *replaced(good, a2=rope(**kw))) == status, kw
+    for at, status in ((dict(a0=shape(head_dim=64)), UNSUP), (dict(a3=0), BAD), (dict(a3=8193), BAD), (dict(a4=FAKE + 1), BAD),
+                       (dict(a5=None), BAD), (dict(a12=None), BAD), (dict(a12=FAKE), BAD), (dict(a8=None), BAD),
+                       (dict(a9=None), BAD), (dict(a10=None), BAD), (dict(a11=None), BAD),
+                       (dict(a9=(FAKE, 1 << 22, 1 << 13, 128)), BAD), (dict(a11=(FAKE, 1 << 20, 1 << 13, 128)), BAD),
+                       (dict(a0=shape(batch=8000, t_cap=1 << 20), a1=pages(table_ld=1 << 14), a3=1 << 20), UNSUP)):
+        assert rc_of(f, *replaced(good, **at)) == status, at
+    for r in ROWS:
+        for at in ("a6", "a7", "a8", "a9", "a10", "a11"):
+            assert rc_of(f, *replaced(good, **{at: r})) == BAD, (at, r)
+    for r in OVERLAP:
+        for at in ("a9", "a11"):
+            assert rc_of(f, *replaced(good, **{at: r})) == BAD, (at, r)
+
+
+def test_select_refusals():
+    f, s = sp.sparda_paged_select, shape()
+    good = [s, pages(k=None, v=None, page_ld=0), FAKE, FAKE, 8000, FAKE, FAKE, FAKE, 1 << 40]
+    for kw, status in PAGES + ((dict(k_cmp=None), BAD), (dict(k_cmp=FAKE + 2), BAD), (dict(page_size=32, table_ld=256), UNSUP)):
+        assert rc_of(f, *replaced(good, a1=pages(**kw))) == status, kw
+    for at, status in ((dict(a0=shape(block_size=32)), UNSUP), (dict(a2=None), BAD), (dict(a2=FAKE + 8), BAD), (dict(a3=None), BAD),
+                       (dict(a4=0), BAD), (dict(a4=8193), BAD), (dict(a4=-1 << 62), BAD), (dict(a5=None), BAD),
+                       (dict(a6=FAKE + 1), BAD), (dict(a7=None), WS), (dict(a7=FAKE + 4), WS), (dict(a8=1024), WS)):
+        assert rc_of(f, *replaced(good, **at)) == status, at
+
+
+def test_attn_refusals():
+    f, s = sp.sparda_paged_attn, shape()
+    good = [s, pages(k_cmp=None), FAKE, FAKE, 8000, FAKE, FAKE, 0.088, FAKE, FAKE, 1 << 40]
+    for kw, status in PAGES + ((dict(k=None), BAD), (dict(v=None), BAD), (dict(v=FAKE + 8), BAD),
+                               (dict(page_ld=8 * 64 * 128 - 8), BAD), (dict(page_ld=8 * 64 * 128 + 1), BAD)):
+        assert rc_of(f, *replaced(good, a1=pages(**kw))) == status, kw
+    for at, status in ((dict(a0=shape(group_size=17)), UNSUP), (dict(a2=None), BAD), (dict(a3=FAKE + 2), BAD), (dict(a4=0), BAD),
+                       (dict(a4=8193), BAD), (dict(a5=None), BAD), (dict(a6=None), BAD), (dict(a5=FAKE + 1), BAD),
+                       (dict(a7=NAN), BAD), (dict(a7=INF), BAD), (dict(a7=3e38), BAD), (dict(a8=None), BAD), (dict(a8=FAKE + 8), BAD),
+                       (dict(a9=None), WS), (dict(a9=FAKE + 4), WS), (dict(a10=1024), WS)):
+        assert rc_of(f, *replaced(good, **at)) == status, at
+
+
+def test_workspace_sizes():
+    w = sp.sparda_workspace_size
+    s = shape()
+    assert w(s, sp.SPARDA_OP_PAGED_SELECT, 1, 63) == 0
+    assert w(s, sp.SPARDA_OP_PAGED_SELECT, 1, 8191) == 16 * 128 * 4  # 125 candidates, rounded up to 16 bytes
+    assert w(s, sp.SPARDA_OP_PAGED_ATTN, 1, 0) == w(s, sp.SPARDA_OP_PAGED_ATTN, 1, 8191) > 0
+    for op in (sp.SPARDA_OP_PAGED_SELECT, sp.SPARDA_OP_PAGED_ATTN):
+        assert rc_of(w, s, op, 2, 100) == BAD
+        assert rc_of(w, s, op, 1, 8192) == BAD
+        assert rc_of(w, s, op, 1, -1) == BAD
+
+
+def test_handles_check_their_tensors():
+    k = torch.zeros(4, 2, 64, 128, dtype=torch.bfloat16)
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    both = torch.zeros(4, 2, 2, 64, 128, dtype=torch.bfloat16)
+    c = sp.SpardaPages(64, table, both[:, 0], both[:, 1]).c
+    assert (c.n_pages, c.table_ld, c.page_ld) == (4, 3, 2 * 2 * 64 * 128)
+    for args in ((64, table), (64, table, k, None), (64, table, k, k[:3]), (64, table.long(), k, k), (64, table.t(), k, k),
+                 (64, table, k.float(), k), (64, table, k.transpose(1, 2), k), (64, table, k, both[:, 0])):
+        with pytest.raises(ValueError):
+            sp.SpardaPages(*args)
+    for freq in (torch.zeros(64), torch.zeros(63, dtype=torch.float64), torch.zeros(128, dtype=torch.float64)[::2]):
+        with pytest.raises(ValueError):
+            sp.SpardaRope(128, sp.SPARDA_ROPE_HALF, freq)
+    r = sp.SpardaRope(128, sp.SPARDA_ROPE_HALF, FAKE)
+    x, pos = torch.zeros(1, 2, 3, 128), torch.zeros(3, dtype=torch.int32)
+    for bad in (x.bfloat16(), x[:, :1], x.transpose(2, 3)):
+        with pytest.raises(ValueError):
+            sp.sparda_rotate(r, sp.SPARDA_F32, 1, 2, 3, bad, pos, 0, x)
+    with pytest.raises(ValueError):  # memory of the host
+        sp.sparda_rotate(r, sp.SPARDA_F32, 1, 2, 3, x, pos, 0, x)
+
+
+def test_frequencies():
+    n = 64
+    plain = [10000.0 ** (-j / n) for j in range(n)]
+    f, s = sp.sparda_rope_freqs(128, 10000.0)
+    assert s == 1.0 and torch.allclose(f, torch.tensor(plain, dtype=torch.float64), rtol=1e-14, atol=0)
+    f, s = sp.sparda_rope_freqs(128, 10000.0, sp.SPARDA_ROPE_LINEAR, 4.0)
+    assert s == 1.0 and torch.allclose(f, torch.tensor(plain, dtype=torch.float64) / 4, rtol=1e-14, atol=0)
+    f, s = sp.sparda_rope_freqs(128, 10000.0, sp.SPARDA_ROPE_BASE, 4.0)
+    assert s == 1.0 and f[0] == 1.0 and math.isclose(float(f[-1]), plain[-1] / 4, rel_tol=1e-12)  # slowest pair: divided
+    f, s = sp.sparda_rope_freqs(128, 10000.0, sp.SPARDA_ROPE_BANDS, 4.0, 8192, 1.0, 32.0)
+    assert math.isclose(s, 1 + 0.1 * math.log(4.0), rel_tol=1e-6)
+    for j, x in enumerate(plain):
+        turns = 8192 * x / (2 * math.pi)
+        keep = min(1.0, max(0.0, (turns - 1) / 31))
+        assert math.isclose(float(f[j]), x * keep + x / 4 * (1 - keep), rel_tol=1e-12)
+    div = [1.0 + j for j in range(n)]
+    f, s = sp.sparda_rope_freqs(128, 40000.0, sp.SPARDA_ROPE_FACTORS, 4.0, 32768, factors=div)
+    assert math.isclose(s, math.sqrt(1 + math.log(4.0) / math.log(32768)), rel_tol=1e-6)
+    assert torch.allclose(f * torch.tensor(div, dtype=torch.float64), torch.tensor([40000.0 ** (-j / n) for j in range(n)],
+                                                                                  dtype=torch.float64), rtol=1e-13, atol=0)
+    # a factor of 1 changes nothing
+    for kind in (sp.SPARDA_ROPE_LINEAR, sp.SPARDA_ROPE_BASE, sp.SPARDA_ROPE_BANDS):
+        f, s = sp.sparda_rope_freqs(128, 10000.0, kind, 1.0, 8192)
+        assert s == 1.0 and torch.allclose(f, torch.tensor(plain, dtype=torch.float64), rtol=1e-13, atol=0)
+    g = sp.sparda_rope_freqs
+    for args, status in (((0, 1e4), BAD), ((130, 1e4), BAD), ((17, 1e4), BAD), ((24, 1e4), UNSUP), ((128, 1.0), BAD), ((128, NAN), BAD),
+                         ((128, INF), BAD), ((128, 1e4, 5), BAD), ((128, 1e4, -1), BAD), ((128, 1e4, 1, 0.5), BAD),
+                         ((128, 1e4, 1, NAN), BAD), ((128, 1e4, 3, 4.0, 1.0), BAD), ((128, 1e4, 3, 4.0, 8192, 2.0, 2.0), BAD),
+                         ((128, 1e4, 3, 4.0, 8192, -1.0, 2.0), BAD), ((128, 1e4, 3, 4.0, 8192, 1.0, INF), BAD),
+                         ((128, 1e4, 4, 4.0, 8192), BAD), ((128, 1e4, 4, 4.0, 8192, 1.0, 32.0, [0.0] * 64), BAD),
+                         ((128, 1e4, 4, 4.0, 8192, 1.0, 32.0, [NAN] * 64), BAD)):
+        assert rc_of(g, *args) == status, args
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_reference_rotation_keeps_relative_positions(pairs):
+    gen = torch.Generator().manual_seed(3)
+    q, k = (torch.randn(1, 128, generator=gen, dtype=torch.float64) for _ in range(2))
+    freq = torch.tensor([10000.0 ** (-j / 32) for j in range(32)], dtype=torch.float64)
+    at = lambda x, p: ref.turn(x, torch.tensor([p]), freq, 64, pairs, 1.0)[0]  # noqa: E731
+    assert math.isclose(float((at(q, 7) * at(k, 3)).sum()), float((at(q, 1004) * at(k, 1000)).sum()), rel_tol=1e-9)
+    assert torch.allclose(ref.turn(at(q, 9), torch.tensor([9]), freq, 64, pairs, 1.0, back=True)[0], q)
+    assert torch.equal(at(q, 9)[:, 64:], q[:, 64:])
+
+
+def test_reference_gradient_against_differences():
+    """The transposed rotation is the gradient of the rotation."""
+    gen = torch.Generator().manual_seed(4)
+    x, g = (torch.randn(2, 128, generator=gen, dtype=torch.float64) for _ in range(2))
+    freq, pos, eps = torch.rand(48, generator=gen, dtype=torch.float64), torch.tensor([5, 900]), 1e-5
+    got = ref.turn(g, pos, freq, 96, True, 1.3, back=True)[0]
+    for i in (0, 1, 50, 95, 96, 127):
+        d = torch.zeros_like(x)
+        d[:, i] = eps
+        diff = (ref.turn(x + d, pos, freq, 96, True, 1.3)[0] - ref.turn(x - d, pos, freq, 96, True, 1.3)[0]) / (2 * eps)
+        assert torch.allclose((diff * g).sum(1), got[:, i], atol=1e-8)
+
+
+def test_reference_selection_and_attention_by_hand():
+    keys = torch.zeros(6, 128)
+    keys[:, 0] = torch.tensor([9.0, 1.0, 3.0, 3.0, 2.0, 8.0])
+    f = torch.zeros(128)
+    f[0] = 1.0
+    # 6 complete blocks and one token: block 6 is the query's, block 5 local, block 0 initial; 2 and 3 tie
+    assert ref.selection(f, keys, 385, 4, 1, 2, (64, 64)) == [0, 2, 5, 6]
+    assert ref.selection(f, keys, 385, 5, 1, 2, (64, 64)) == [0, 2, 3, 5, 6]
+    k = torch.zeros(2, 1, 16, 128)
+    v = torch.arange(32.0).view(2, 1, 16, 1).expand(2, 1, 16, 128)
+    table = torch.tensor([[1, 0]], dtype=torch.int32)
+    o, _ = ref.attn(torch.zeros(1, 1, 128), k, v, table, torch.tensor([18]), 16, None, None, 1.0)
+    assert torch.allclose(o, torch.full_like(o, (sum(range(16, 32)) + 0 + 1) / 18))
+    table[0, 0] = 2  # no page: only the last two tokens are left
+    o, _ = ref.attn(torch.zeros(1, 1, 128), k, v, table, torch.tensor([18]), 16, None, None, 1.0)
+    assert torch.allclose(o, torch.full_like(o, 0.5))
