@@ -219,9 +219,10 @@ def _run_own(s):
     if "shape" not in s:  # what a program keeps from call to call: the shape, the rotation, the layer's pages
         if c["op"] != "rotate":
             cap, grid = _t_cap(c), c.get("grid", 64)
+            n_init, n_local = c.get("n_init", 1), c.get("n_local", 2)
             s["shape"] = sp.SpardaShape(batch=c["batch"], n_kv_heads=c["kvh"], group_size=c.get("g", 1),
-                                        k_total=c.get("k") or 3, t_cap=cap, nc_cap=0, n_init=c.get("n_init", 1),
-                                        n_local=c.get("n_local", 2), cmp_kernel=grid, cmp_stride=16 if grid == 32 else 64)
+                                        k_total=c.get("k") or n_init + n_local, t_cap=cap, nc_cap=0, n_init=n_init,
+                                        n_local=n_local, cmp_kernel=grid, cmp_stride=16 if grid == 32 else 64)
             s["pages"] = sp.SpardaPages(c["page"], s["table"], s.get("k"), s.get("v"), s.get("kc"))
         else:
             s["shape"] = None
