@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass, field
 
 import torch
@@ -81,15 +82,21 @@ class SpardaShape:
     def n_q_heads(self) -> int:
         return self.n_kv_heads * self.group_size
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_c", None)  # the C struct below is of other values
+
     def c(self) -> _CShape:
+        c = self._c
+        if c is None:
+            c = self._make()
+            object.__setattr__(self, "_c", c)
+        return c
+
+    def _make(self) -> _CShape:
         return _CShape(ctypes.sizeof(_CShape), self.batch, self.n_kv_heads, self.group_size, self.head_dim,
                        self.block_size, self.cmp_kernel, self.cmp_stride, self.n_init, self.n_local, self.k_total,
                        self.t_cap, self.nc_cap)
-
-
-class _CRows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("ld_batch", ctypes.c_int64), ("ld_head", ctypes.c_int64),
-                ("ld_token", ctypes.c_int64)]
 
 
 class _CRope(ctypes.Structure):
@@ -177,7 +184,7 @@ def load() -> ctypes.CDLL:
         lib.sparda_tree_verify.argtypes = [S, i32, i32, i64, i32, P, P, P, P, P, P, P, P, P, sz, P]
         lib.sparda_tree_verify_workspace_size.argtypes = [S, i32, i32, ctypes.POINTER(sz)]
         lib.sparda_tree_commit.argtypes = [S, i32, P, P, P, i32, P, P, P, P, P, P, P]
-        R, W, G = ctypes.POINTER(_CRope), ctypes.POINTER(_CRows), ctypes.POINTER(_CPages)
+        R, W, G = ctypes.POINTER(_CRope), ctypes.c_char_p, ctypes.POINTER(_CPages)  # W: packed bytes (_rows)
         f64 = ctypes.c_double
         lib.sparda_rope_freqs.argtypes = [i32, f64, i32, f64, f64, f64, f64, P, P, ctypes.POINTER(ctypes.c_float)]
         lib.sparda_rotate.argtypes = [R, i32, i32, i32, i64, W, P, i64, W, i32, P]
@@ -233,23 +240,29 @@ def _expect(x, name: str, dtype, numel: int):
 
 def _here(*tensors):
     """The tensors are in the memory of the current device, whose stream the call goes to."""
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2  # (-1: a tensor in host memory)
+    dev = _device() if torch.cuda.is_initialized() else -2  # (-1: a tensor in host memory)
     for x in tensors:
         if x is not None and not isinstance(x, (int, tuple)) and x.get_device() != dev:
             raise ValueError(f"a tensor is on {x.device}, the current device is {'cuda:%d' % dev if dev >= 0 else 'not in use'}")
 
 
-def _rows(x, name: str, shape, dtype=None):
-    """struct sparda_rows of a tensor [B][heads][tokens][128] of any strides, or of (address, ld_batch, ld_head, ld_token)."""
+_pack_rows = struct.Struct("=Qqqq").pack  # struct sparda_rows
+
+
+def _rows(x, name: str, shape, dtype):
+    """struct sparda_rows of a tensor [B][heads][tokens][128] of any strides, or of (address, ld_batch, ld_head, ld_token).
+    Packed bytes: a ctypes structure costs 1.7 us, and an append has six."""
     if x is None:
         return None
     if isinstance(x, tuple):
-        return ctypes.byref(_CRows(*x))
-    if x.shape != shape or (dtype is not None and x.dtype != dtype) or x.stride(3) != 1:
+        return _pack_rows(x[0] or 0, *x[1:])
+    ld = x.stride()
+    if x.shape != shape or x.dtype != dtype or ld[3] != 1:
         raise ValueError(f"{name}: {tuple(shape)} of {dtype} expected, its last dimension dense")
-    return ctypes.byref(_CRows(x.data_ptr(), x.stride(0), x.stride(1), x.stride(2)))
+    return _pack_rows(x.data_ptr(), ld[0], ld[1], ld[2])
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 # The current stream's handle without a Stream object around it (0.4 us instead of 2.9 us per call).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -257,7 +270,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 def _stream(stream):
     if stream is None:
         if _raw_stream is not None and torch.cuda.is_initialized():
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
     if isinstance(stream, int):
         return stream
