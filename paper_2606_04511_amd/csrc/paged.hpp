@@ -126,8 +126,10 @@ inline PagedPlan paged_attn_plan(int64_t rows, int64_t t_max, int32_t k_total, b
 }
 // Two partial results per wavefront, each per head: 128 sums, the maximum and the denominator (4 floats apart).
 constexpr int kPartFloats = 132;
-inline size_t paged_attn_ws(int32_t group_size) {
-  return (size_t)kPagedMaxWgs * kPagedWaves * 2 * (size_t)group_size * kPartFloats * sizeof(float);
+// Before them a flag per workgroup and the starts of the sequences: 4 bytes each.
+__host__ __device__ inline int64_t paged_parts_at(int64_t batch) { return (kPagedMaxWgs + batch + 1 + 63) & ~(int64_t)63; }
+inline size_t paged_attn_ws(int64_t batch, int32_t group_size) {
+  return ((size_t)paged_parts_at(batch) + (size_t)kPagedMaxWgs * kPagedWaves * 2 * (size_t)group_size * kPartFloats) * sizeof(float);
 }
 
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t stream);

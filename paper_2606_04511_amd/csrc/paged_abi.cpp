@@ -279,7 +279,7 @@ int sparda_paged_attn(const sparda_shape* shape, const sparda_pages* pages, cons
   if ((sel == nullptr) != (cnt == nullptr)) return fail(SPARDA_ERR_INVALID_ARG, "sel and cnt: both or neither");
   if (sel && ((rc = check_dev(sel, "sel", 2)) || (rc = check_dev(cnt, "cnt", 2)))) return rc;
   if (!std::isfinite(sm_scale * 1.44269504088896340736f)) return fail(SPARDA_ERR_INVALID_ARG, "sm_scale is not finite");
-  if ((rc = check_ws(ws, ws_bytes, sparda::paged_attn_ws(shape->group_size)))) return rc;
+  if ((rc = check_ws(ws, ws_bytes, sparda::paged_attn_ws(shape->batch, shape->group_size)))) return rc;
   a.q = static_cast<const uint16_t*>(q);
   a.t_ctx = t_ctx;
   a.t_max = t_max;

@@ -2,9 +2,10 @@
 // context, for sequences of different lengths whose K and V lie in pages (paper Sec. 4.1, Eq. 5).
 //
 // The work is a line of units of 32 tokens, row after row (a row is a sequence's KV head with its G query heads), cut into
-// equal pieces, one per wavefront, whatever the lengths are.  A wavefront goes over its piece once with a running maximum
-// and sum per head; a piece that holds a whole row writes its output, any other leaves a partial result per row, which the
-// eight wavefronts of a workgroup join in LDS where one row fills the workgroup, and paged_join_kernel joins the rest.
+// equal pieces, one per wavefront, whatever the lengths are.  The eight wavefronts of a workgroup whose pieces lie in one or
+// two rows divide those rows instead and join their results in LDS.  A wavefront goes over its units once with a running
+// maximum and sum per head.  A row that ends up whole is written; the results of the others go to the workspace and
+// paged_join_kernel joins them.
 //
 // A unit is two slices of 16 tokens, the smallest page.  S^T = K Q^T on the matrix cores with 16 tokens as rows and the
 // heads as columns: K goes through 8 KiB of the wavefront's LDS (whole rows in, fragments of 16 bytes out, swizzled).
@@ -23,97 +24,111 @@ namespace {
 
 constexpr int kThreads = kPagedWaves * 64;
 
-struct Line {        // a workgroup's view of the line of units
-  int64_t total;     // units
-  int64_t piece;     // units of a wavefront
-};
-
-// A row's place on the line.
+// A row's place on the line.  A call has fewer than 2^32 units (65535 rows of 65536).
 struct RowAt {
   int b, h;
-  int64_t t;         // tokens of the sequence
-  int64_t u0, units; // its first unit on the line, its units
+  int64_t t;          // tokens of the sequence
+  uint32_t u0, units; // its first unit on the line, its units
+  __device__ uint32_t end() const { return u0 + units; }
 };
 
 __device__ __forceinline__ int64_t attn_context(const PagedAttnArgs& a, int b) {
   const int64_t t = a.t_ctx[b];
   return t > a.t_max ? a.t_max : t;
 }
-__device__ __forceinline__ int64_t dense_units(int64_t t) { return t > 0 ? (t + 31) >> 5 : 0; }
+__device__ __forceinline__ uint32_t dense_units(int64_t t) { return t > 0 ? (uint32_t)((t + 31) >> 5) : 0u; }
 
-// Units per KV head of the sequences before each thread's, and of all (a thread has `per` consecutive sequences); the
-// starts go to pre[0 .. kThreads).  Every thread of the workgroup must call it.
-template <int kT>
-__device__ __forceinline__ int64_t scan_lengths(const PagedAttnArgs& a, int per, int64_t* pre, int64_t* sums) {
+// Where the sequences of a dense call begin on the line, in units per KV head.  Up to 64 sequences: lane i holds the start
+// of sequence i, formed by each wavefront on its own.  More: thread i has `per` consecutive sequences and its start is
+// pre[i] in LDS.  Every thread of the workgroup must call it.
+struct Starts {
+  uint32_t mine;   // per KV head
+  uint32_t total;
+};
+__device__ __forceinline__ Starts scan_lengths(const PagedAttnArgs& a, int per, uint32_t* pre, uint32_t* sums) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int64_t mine = 0;
+  uint32_t mine = 0;
+  if (per == 0) {
+    mine = lane < a.batch ? dense_units(attn_context(a, lane)) : 0u;
+    const uint32_t incl = (uint32_t)wave_incl_scan_dpp((int)mine);
+    return {incl - mine, (uint32_t)readlane_i((int)incl, 63)};
+  }
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
     if (b < a.batch) mine += dense_units(attn_context(a, b));
   }
-  int64_t incl = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up((long long)incl, d, 64);
-    if (lane >= d) incl += y;
-  }
+  const uint32_t incl = (uint32_t)wave_incl_scan_dpp((int)mine);
   if (lane == 63) sums[wave] = incl;
   __syncthreads();
-  int64_t before = 0, total = 0;
-  for (int w = 0; w < kT / 64; ++w) {
+  uint32_t before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kPagedWaves; ++w) {
     if (w < wave) before += sums[w];
     total += sums[w];
   }
   pre[tid] = before + incl - mine;
   __syncthreads();
-  return total;
+  return {before + incl - mine, total};
 }
 
-// The row that holds unit u (u < total) of a dense call's line.
-template <int kT>
-__device__ __forceinline__ RowAt dense_row(const PagedAttnArgs& a, int per, const int64_t* pre, int64_t u) {
+// The row that holds unit u (one of the line's) of a dense call.
+__device__ __forceinline__ RowAt dense_row(const PagedAttnArgs& a, int per, const Starts& st, const uint32_t* pre, uint32_t u) {
   const int lane = threadIdx.x & 63;
-  int n = 0;  // starts at or before u: the last of them holds it
+  const uint32_t H = (uint32_t)a.n_kv_heads;
+  int b;
+  uint32_t at;
+  if (per == 0) {  // starts at or before u: the last of them holds it
+    b = (int)__popcll(__ballot(lane < a.batch && st.mine * H <= u)) - 1;
+    at = (uint32_t)readlane_i((int)st.mine, b) * H;
+  } else {
+    int n = 0;
 #pragma unroll
-  for (int i = 0; i < kT / 64; ++i) n += (int)__popcll(__ballot(pre[64 * i + lane] * a.n_kv_heads <= u));
-  int b = (n - 1) * per;
-  int64_t at = pre[n - 1] * a.n_kv_heads;
+    for (int i = 0; i < kPagedWaves; ++i) n += (int)__popcll(__ballot(pre[64 * i + lane] * H <= u));
+    b = (n - 1) * per;
+    at = pre[n - 1] * H;
+  }
   for (;; ++b) {
-    const int64_t t = attn_context(a, b), units = dense_units(t);
-    if (u < at + units * a.n_kv_heads || b + 1 >= a.batch) {
-      const int h = units > 0 ? (int)((u - at) / units) : 0;
-      return {b, h, t, at + h * units, units};
+    const int64_t t = attn_context(a, b);
+    const uint32_t units = dense_units(t);
+    if (u < at + units * H || b + 1 >= a.batch) {
+      const uint32_t h = units > 0 ? (u - at) / units : 0u;
+      return {b, (int)h, t, at + h * units, units};
     }
-    at += units * a.n_kv_heads;
+    at += units * H;
   }
 }
-// The next row that has units.
-__device__ __forceinline__ void next_dense_row(const PagedAttnArgs& a, RowAt* r) {
-  r->u0 += r->units;
-  if (++r->h < a.n_kv_heads) return;
-  r->h = 0;
-  while (++r->b < a.batch) {
-    r->t = attn_context(a, r->b);
-    r->units = dense_units(r->t);
-    if (r->units > 0) return;
+// The row behind r that has units.
+__device__ __forceinline__ RowAt next_dense_row(const PagedAttnArgs& a, RowAt r) {
+  r.u0 += r.units;
+  if (++r.h < a.n_kv_heads) return r;
+  r.h = 0;
+  while (++r.b < a.batch) {
+    r.t = attn_context(a, r.b);
+    r.units = dense_units(r.t);
+    if (r.units > 0) return r;
   }
-  r->units = (int64_t)1 << 60;  // past the line
+  r.units = 0;  // past the line
+  return r;
 }
-
-__device__ __forceinline__ RowAt sparse_row(const PagedAttnArgs& a, int64_t row_units, int64_t u) {
-  const int64_t row = u / row_units;
-  const int b = (int)(row / a.n_kv_heads), h = (int)(row % a.n_kv_heads);
+__device__ __forceinline__ RowAt sparse_row(const PagedAttnArgs& a, uint32_t row_units, uint32_t u) {
+  const uint32_t row = u / row_units;
+  const int b = (int)(row / (uint32_t)a.n_kv_heads), h = (int)(row % (uint32_t)a.n_kv_heads);
   return {b, h, attn_context(a, b), row * row_units, row_units};
 }
 
-// Does the piece of workgroup [w0, w1) lie in one row?  Then its wavefronts join in LDS.
-__device__ __forceinline__ bool shares_row(const RowAt& r, int64_t w0, int64_t w1) {
-  return r.u0 <= w0 && w1 <= r.u0 + r.units;
+// The workspace: whether the wavefronts of workgroup i share their rows; where sequence b begins on the line (dense calls);
+// the partial results, two per wavefront.
+__device__ __forceinline__ int32_t* shared_flags(const PagedAttnArgs& a) { return reinterpret_cast<int32_t*>(a.ws); }
+__device__ __forceinline__ uint32_t* line_starts(const PagedAttnArgs& a) {
+  return reinterpret_cast<uint32_t*>(a.ws) + kPagedMaxWgs;
+}
+__device__ __forceinline__ float* partial(const PagedAttnArgs& a, int64_t slot, int head) {
+  return a.ws + paged_parts_at(a.batch) + (slot * a.group_size + head) * kPartFloats;
 }
 
-// Partial result `slot` of head i.
-__device__ __forceinline__ float* partial(const PagedAttnArgs& a, int64_t slot, int head) {
-  return a.ws + (slot * a.group_size + head) * kPartFloats;
+// Units of a wavefront's piece.
+__device__ __forceinline__ uint32_t line_piece(uint32_t total, uint32_t n_wgs) {
+  return (total + n_wgs * kPagedWaves - 1) / (n_wgs * kPagedWaves);
 }
 
 // A wavefront's running softmax: lane (g, c) holds elements 32 g + 8 r + j of head c in acc[j][r], the denominators of its
@@ -125,7 +140,7 @@ struct Running {
 
 // The wavefront's units [u0, u1) of row r (counted within the row).
 template <bool kSparse>
-__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, int64_t u0, int64_t u1, char* kbuf, Running* run) {
+__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, int u0, int u1, char* kbuf, Running* run) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) run->acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -148,31 +163,31 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, i
     cnt = a.cnt[row];
     cnt = cnt < 0 ? 0 : cnt > a.k_total ? a.k_total : cnt;
     // a list that ascends strictly names no block twice
-    const int last = (int)min((int64_t)cnt, (u1 + 1) >> 1);
+    const int last = min(cnt, (u1 + 1) >> 1);
     for (int i0 = 0; i0 < last; i0 += 64) {
       const int i = i0 + lane;
       if (__ballot(i > 0 && i < last && sel[min(i, last - 1)] <= sel[max(min(i, last - 1) - 1, 0)]) != 0ull) ascending = false;
     }
   }
-  for (int64_t hb = u0; hb < u1; hb += 32) {
+  for (int hb = u0; hb < u1; hb += 32) {
     // lane i: slice i of the next 32 units; lim: its tokens
     int64_t tok = 0, off = 0;
     int lim = 0;
-    const int64_t u = hb + (lane >> 1);
+    const int u = hb + (lane >> 1);
     if constexpr (kSparse) {
-      const int64_t e = u >> 1;
+      const int e = u >> 1;
       if (u < u1 && e < cnt) {
         const int blk = sel[e];
-        tok = (int64_t)blk * 64 + ((int)u & 1) * 32 + (lane & 1) * 16;
+        tok = (int64_t)blk * 64 + (u & 1) * 32 + (lane & 1) * 16;
         if (blk >= 0 && tok < r.t) {
           lim = (int)min(r.t - tok, (int64_t)16);
           if (!ascending)
-            for (int64_t x = 0; x < e; ++x)
+            for (int x = 0; x < e; ++x)
               if (sel[x] == blk) lim = 0;
         }
       }
     } else {
-      tok = u * 32 + (lane & 1) * 16;
+      tok = (int64_t)u * 32 + (lane & 1) * 16;
       if (u < u1 && tok < r.t) lim = (int)min(r.t - tok, (int64_t)16);
     }
     if (lim > 0) {
@@ -340,187 +355,253 @@ __device__ __forceinline__ float join_weight(float m, float top) {
 }
 
 template <bool kSparse>
-__global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a, int64_t row_units, int per) {
+__global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a, uint32_t row_units, int per) {
   __shared__ __align__(16) char kbuf[kPagedWaves][32 * 256];
-  __shared__ int64_t pre[kSparse ? 1 : kThreads], sums[kPagedWaves];
+  __shared__ uint32_t pre[kSparse ? 1 : kThreads], sums[kPagedWaves];
   __shared__ float stat[kPagedWaves][16][2];
-  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Line line;
+  Starts st = {0u, 0u};
+  uint32_t total;
   if constexpr (kSparse) {
-    line.total = (int64_t)a.batch * a.n_kv_heads * row_units;
+    total = (uint32_t)(a.batch * a.n_kv_heads) * row_units;
   } else {
-    line.total = scan_lengths<kThreads>(a, per, pre, sums) * a.n_kv_heads;
+    st = scan_lengths(a, per, pre, sums);
+    total = st.total * (uint32_t)a.n_kv_heads;
+    if (blockIdx.x == 0) {  // for the join
+      uint32_t* starts = line_starts(a);
+      const int n = per == 0 ? 1 : per;
+      uint32_t at = st.mine;
+      for (int i = 0; i < n; ++i) {
+        const int b = tid * n + i;
+        if (b >= a.batch || (per == 0 && wave > 0)) break;
+        starts[b] = at;
+        at += dense_units(attn_context(a, b));
+      }
+      if (tid == 0) starts[a.batch] = st.total;
+    }
     // rows without tokens are on no piece
-    for (int64_t b = blockIdx.x; b < a.batch; b += gridDim.x)
-      if (attn_context(a, (int)b) <= 0) {
-        uint4* o = reinterpret_cast<uint4*>(a.o + b * a.n_kv_heads * a.group_size * kHeadDim);
+    for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+      if (attn_context(a, b) <= 0) {
+        uint4* o = reinterpret_cast<uint4*>(a.o + (int64_t)b * a.n_kv_heads * a.group_size * kHeadDim);
         for (int i = tid; i < a.n_kv_heads * a.group_size * (kHeadDim / 8); i += kThreads) o[i] = make_uint4(0u, 0u, 0u, 0u);
       }
   }
-  const int64_t pieces = (int64_t)gridDim.x * kPagedWaves;
-  line.piece = (line.total + pieces - 1) / pieces;
-  const int64_t w0 = (int64_t)blockIdx.x * kPagedWaves * line.piece;
-  if (w0 >= line.total) return;
-  const int64_t w1 = min(w0 + kPagedWaves * line.piece, line.total);
-  const int64_t p0 = w0 + wave * line.piece, p1 = min(p0 + line.piece, line.total);
+  const uint32_t piece = line_piece(total, gridDim.x);
+  const uint32_t w0 = blockIdx.x * kPagedWaves * piece;
+  if (w0 >= total) return;
+  const uint32_t w1 = total - w0 < kPagedWaves * piece ? total : w0 + kPagedWaves * piece;
+  auto row_at = [&](uint32_t u) {
+    if constexpr (kSparse)
+      return sparse_row(a, row_units, u);
+    else
+      return dense_row(a, per, st, pre, u);
+  };
+  auto next_row = [&](const RowAt& r) {
+    if constexpr (kSparse)
+      return sparse_row(a, row_units, r.end());
+    else
+      return next_dense_row(a, r);
+  };
   Running run;
-  RowAt r = kSparse ? sparse_row(a, row_units, w0) : dense_row<kThreads>(a, per, pre, w0);
-  if (shares_row(r, w0, w1)) {
-    const int64_t u0 = min(p0, w1), u1 = max(p1, u0);  // the last piece may be short, or empty
-    attend<kSparse>(a, r, u0 - r.u0, u1 - r.u0, kbuf[wave], &run);
-    // ---- the wavefronts' results joined: a head's 128 sums of a wavefront in its K buffer
-    float* mine = reinterpret_cast<float*>(kbuf[wave]);
-    __builtin_amdgcn_wave_barrier();
-    const int g = lane >> 4;
+  RowAt r = row_at(w0);
+  RowAt second = r;
+  if (r.end() < w1) second = next_row(r);
+  const bool share = second.end() >= w1;
+  if (tid == 0) shared_flags(a)[blockIdx.x] = share ? 1 : 0;
+  if (share) {
+    // one row or two: the wavefronts divide each, and their results join in LDS (a head's 128 sums of a wavefront in its
+    // K buffer, 16 bytes at a time; piece x of head c lies at x ^ 2 c, free of bank conflicts)
+    for (uint32_t u = w0;;) {
+      const uint32_t end = r.end() < w1 ? r.end() : w1, n = end - u, each = (n + kPagedWaves - 1) / kPagedWaves;
+      const uint32_t v0 = wave * each < n ? wave * each : n, v1 = v0 + each < n ? v0 + each : n;
+      attend<kSparse>(a, r, (int)(u - r.u0 + v0), (int)(u - r.u0 + v1), kbuf[wave], &run);
+      char* mine = kbuf[wave] + c * 512;
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) mine[c * 128 + 32 * g + 8 * x + j] = run.acc[j][x];
-    if (g == 0) {
-      stat[wave][c][0] = run.m;
-      stat[wave][c][1] = run.l;
-    }
-    __syncthreads();
-    const bool whole = r.u0 == w0 && r.units == w1 - w0;
-    for (int i = tid; i < a.group_size * 128; i += kThreads) {
-      const int head = i >> 7, d = i & 127;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, stat[w][head][0]);
-      float sum = 0.f, l = 0.f;
-#pragma unroll
-      for (int w = 0; w < kPagedWaves; ++w) {
-        const float f = join_weight(stat[w][head][0], top);
-        sum = fmaf(f, reinterpret_cast<const float*>(kbuf[w])[i], sum);
-        l = fmaf(f, stat[w][head][1], l);
+      for (int x = 0; x < 4; ++x) {
+        *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x) ^ (2 * c))) = f32x4{run.acc[0][x], run.acc[1][x], run.acc[2][x], run.acc[3][x]};
+        *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x + 1) ^ (2 * c))) = f32x4{run.acc[4][x], run.acc[5][x], run.acc[6][x], run.acc[7][x]};
       }
-      if (whole) {
-        a.o[(((int64_t)r.b * a.n_kv_heads + r.h) * a.group_size + head) * kHeadDim + d] =
-            f32_to_bf16(l == 0.f ? 0.f : sum / l);
-      } else {
-        float* dst = partial(a, (int64_t)blockIdx.x * kPagedWaves * 2, head);
-        dst[d] = sum;
-        if (d == 0) {
-          dst[128] = top;
-          dst[129] = l;
+      if (g == 0) {
+        stat[wave][c][0] = run.m;
+        stat[wave][c][1] = run.l;
+      }
+      __syncthreads();
+      const bool whole = u == r.u0 && end == r.end();
+      for (int i = tid; i < a.group_size * 32; i += kThreads) {
+        const int head = i >> 5, x = i & 31;
+        float top = -INFINITY, f[kPagedWaves], l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, stat[w][head][0]);
+        f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kPagedWaves; ++w) {
+          f[w] = join_weight(stat[w][head][0], top);
+          l = fmaf(f[w], stat[w][head][1], l);
+          const f32x4 y = *reinterpret_cast<const f32x4*>(kbuf[w] + head * 512 + 16 * (x ^ (2 * head)));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] = fmaf(f[w], y[e], sum[e]);
+        }
+        if (whole) {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          uint16_t* o = a.o + (((int64_t)r.b * a.n_kv_heads + r.h) * a.group_size + head) * kHeadDim + 4 * x;
+          *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
+        } else {
+          float* dst = partial(a, (int64_t)blockIdx.x * kPagedWaves * 2 + (u == w0 ? 0 : 1), head);
+          *reinterpret_cast<f32x4*>(dst + 4 * x) = sum;
+          if (x == 0) *reinterpret_cast<float2*>(dst + 128) = make_float2(top, l);
         }
       }
+      u = end;
+      if (u >= w1) return;
+      r = second;
+      __syncthreads();  // the results have been read
     }
-    return;
   }
+  const uint32_t p0 = w0 + wave * piece, p1 = p0 + piece < w1 ? p0 + piece : w1;
   if (p0 >= p1) return;
-  if constexpr (kSparse)
-    r = sparse_row(a, row_units, p0);
-  else
-    r = dense_row<kThreads>(a, per, pre, p0);
-  for (int64_t u = p0; u < p1;) {
-    const int64_t end = min(r.u0 + r.units, p1);
-    attend<kSparse>(a, r, u - r.u0, end - r.u0, kbuf[wave], &run);
-    if (u == r.u0 && end == r.u0 + r.units)
+  r = row_at(p0);
+  for (uint32_t u = p0;;) {
+    const uint32_t end = r.end() < p1 ? r.end() : p1;
+    attend<kSparse>(a, r, (int)(u - r.u0), (int)(end - r.u0), kbuf[wave], &run);
+    if (u == r.u0 && end == r.end())
       write_row(a, r, run);
     else if (c < a.group_size)
       write_partial(partial(a, ((int64_t)blockIdx.x * kPagedWaves + wave) * 2 + (u == p0 ? 0 : 1), c), run);
     u = end;
-    if (u >= p1) break;
-    if constexpr (kSparse)
-      r = sparse_row(a, row_units, u);
-    else
-      next_dense_row(a, &r);
+    if (u >= p1) return;
+    r = next_row(r);
   }
 }
 
-// Joins the partial results of a row's head, in the order of the line.  One workgroup per (row, head): its wavefronts
-// take the parts in turn, two elements per lane.
-template <bool kSparse>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int64_t row_units, int per, int n_wgs) {
-  __shared__ int64_t pre[256], sums[4];
+// Joins the partial results of a row's head, in the order of the line: kWaves wavefronts per (row, head), two elements per
+// lane, eight results requested at once.
+template <bool kSparse, int kWaves>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, uint32_t row_units, int n_wgs, int n_pairs) {
   __shared__ float acc[4][128], stat[4][2];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t row = blockIdx.x / a.group_size;
-  const int head = (int)(blockIdx.x % a.group_size);
-  RowAt r;
-  r.b = (int)(row / a.n_kv_heads);
-  r.h = (int)(row % a.n_kv_heads);
-  int64_t total;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave % kWaves;
+  const int pair = (int)blockIdx.x * (4 / kWaves) + wave / kWaves;
+  if (pair >= n_pairs) return;
+  const int row = pair / a.group_size, head = pair % a.group_size;
+  uint32_t total, u0, units;
   if constexpr (kSparse) {
-    r.u0 = row * row_units;
-    r.units = row_units;
-    total = (int64_t)a.batch * a.n_kv_heads * row_units;
+    u0 = (uint32_t)row * row_units;
+    units = row_units;
+    total = (uint32_t)(a.batch * a.n_kv_heads) * row_units;
   } else {
-    total = scan_lengths<256>(a, per, pre, sums) * a.n_kv_heads;
-    int64_t before = pre[r.b / per];
-    for (int b = r.b / per * per; b < r.b; ++b) before += dense_units(attn_context(a, b));
-    r.units = dense_units(attn_context(a, r.b));
-    r.u0 = before * a.n_kv_heads + r.h * r.units;
-    if (r.units == 0) return;
+    const int b = row / a.n_kv_heads;
+    const uint32_t* starts = line_starts(a);
+    const uint32_t at = starts[b], next = starts[b + 1];
+    units = next - at;
+    u0 = at * (uint32_t)a.n_kv_heads + (uint32_t)(row % a.n_kv_heads) * units;
+    total = starts[a.batch] * (uint32_t)a.n_kv_heads;
+    if (units == 0) return;
   }
-  const int64_t pieces = (int64_t)n_wgs * kPagedWaves, piece = (total + pieces - 1) / pieces, wg = piece * kPagedWaves;
-  const int64_t first = r.u0 / piece, last = (r.u0 + r.units - 1) / piece;  // wavefronts that hold a part
-  const int64_t g0 = first / kPagedWaves, g1 = last / kPagedWaves;
-  auto joined = [&](int64_t x) { return shares_row(r, x * wg, min((x + 1) * wg, total)); };
-  if (first == last && !joined(g0)) return;  // written by its wavefront
-  if (g0 == g1 && joined(g0) && r.u0 == g0 * wg && r.units == min((g0 + 1) * wg, total) - g0 * wg) return;  // by its workgroup
+  const uint32_t end = u0 + units, piece = line_piece(total, n_wgs), wg = piece * kPagedWaves;
+  const int g0 = (int)(u0 / wg), g1 = (int)((end - 1) / wg);
+  const int32_t* flags = shared_flags(a);
+  if (g0 == g1) {  // written by its workgroup, or by one wavefront?
+    if (flags[g0] != 0 || u0 / piece == (end - 1) / piece) return;
+  }
   float m = -INFINITY, l = 0.f, s0 = 0.f, s1 = 0.f;
-  auto take = [&](int64_t slot) {
-    const float* src = partial(a, slot, head);
-    const float pm = src[128], pl = src[129], x0 = src[2 * lane], x1 = src[2 * lane + 1];
-    const float top = fmaxf(m, pm), f = join_weight(m, top), pf = join_weight(pm, top);
-    s0 = s0 * f + x0 * pf;
-    s1 = s1 * f + x1 * pf;
-    l = l * f + pl * pf;
+  auto take8 = [&](auto slot_of, uint32_t valid) {  // results e whose bit is set
+    float pm[8], pl[8], x0[8], x1[8], top = m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (valid >> e & 1u) {
+        const float* src = partial(a, slot_of(e), head);
+        const float2 x = *reinterpret_cast<const float2*>(src + 2 * lane), y = *reinterpret_cast<const float2*>(src + 128);
+        x0[e] = x.x;
+        x1[e] = x.y;
+        pm[e] = y.x;
+        pl[e] = y.y;
+      } else {
+        x0[e] = x1[e] = pl[e] = 0.f;
+        pm[e] = -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, pm[e]);
+    const float f = join_weight(m, top);
+    s0 *= f;
+    s1 *= f;
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float pf = join_weight(pm[e], top);
+      s0 = fmaf(pf, x0[e], s0);
+      s1 = fmaf(pf, x1[e], s1);
+      l = fmaf(pf, pl[e], l);
+    }
     m = top;
   };
-  for (int64_t x = g0 + wave; x <= g1; x += 4) {
-    if (joined(x)) {
-      take(x * kPagedWaves * 2);
-    } else {
-      for (int64_t w = max(first, x * kPagedWaves); w <= min(last, x * kPagedWaves + kPagedWaves - 1); ++w)
-        take(2 * w + (w * piece >= r.u0 ? 0 : 1));  // slot 0: the part at the piece's beginning
+  for (int x0 = g0 + 8 * part; x0 <= g1; x0 += 8 * kWaves) {
+    const int flag = lane < 8 && x0 + lane <= g1 ? flags[x0 + lane] : -1;
+    const uint32_t joined = (uint32_t)__ballot(flag == 1), apart = (uint32_t)__ballot(flag == 0);
+    // slot 0 holds the result that begins where the piece does
+    if (joined)
+      take8([&](int e) { return (int64_t)(x0 + e) * (kPagedWaves * 2) + ((uint32_t)(x0 + e) * wg >= u0 ? 0 : 1); }, joined);
+    for (uint32_t todo = apart; todo != 0u; todo &= todo - 1u) {
+      const int x = x0 + __builtin_ctz(todo);
+      uint32_t in = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t p0 = (uint32_t)x * wg + e * piece;
+        if (p0 < end && p0 + piece > u0) in |= 1u << e;
+      }
+      take8([&](int e) { return ((int64_t)x * kPagedWaves + e) * 2 + ((uint32_t)x * wg + e * piece >= u0 ? 0 : 1); }, in);
     }
   }
-  acc[wave][2 * lane] = s0;
-  acc[wave][2 * lane + 1] = s1;
-  if (lane == 0) {
-    stat[wave][0] = m;
-    stat[wave][1] = l;
-  }
-  __syncthreads();
-  if (tid < 128) {
-    float top = -INFINITY, sum = 0.f, den = 0.f;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.o + ((int64_t)row * a.group_size + head) * kHeadDim);
+  if constexpr (kWaves == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    out[lane] = pack_bf16(s0 * inv, s1 * inv);
+  } else {
+    *reinterpret_cast<float2*>(&acc[wave][2 * lane]) = make_float2(s0, s1);
+    if (lane == 0) {
+      stat[wave][0] = m;
+      stat[wave][1] = l;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    float top = -INFINITY, y0 = 0.f, y1 = 0.f, den = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w][0]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const float f = join_weight(stat[w][0], top);
-      sum = fmaf(f, acc[w][tid], sum);
+      const float2 x = *reinterpret_cast<const float2*>(&acc[w][2 * lane]);
+      y0 = fmaf(f, x.x, y0);
+      y1 = fmaf(f, x.y, y1);
       den = fmaf(f, stat[w][1], den);
     }
-    a.o[(row * a.group_size + head) * kHeadDim + tid] = f32_to_bf16(den == 0.f ? 0.f : sum / den);
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    out[lane] = pack_bf16(y0 * inv, y1 * inv);
   }
+}
+
+template <bool kSparse>
+hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream) {
+  const int per = a.batch <= 64 ? 0 : (a.batch + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL(paged_attn_kernel<kSparse>, dim3((unsigned)p.n_wgs), dim3(kThreads), 0, stream, a, (uint32_t)p.row_units, per);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.joined) return e;
+  // rows are cut into about n_wgs / rows + 1 results: four wavefronts per head where those are more than eight
+  const int rows = a.batch * a.n_kv_heads, pairs = rows * a.group_size;
+  if (rows * 8 < p.n_wgs)
+    hipLaunchKernelGGL((paged_join_kernel<kSparse, 4>), dim3((unsigned)pairs), dim3(256), 0, stream, a, (uint32_t)p.row_units, p.n_wgs, pairs);
+  else
+    hipLaunchKernelGGL((paged_join_kernel<kSparse, 1>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, a, (uint32_t)p.row_units, p.n_wgs, pairs);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.batch * a.n_kv_heads;
-  const bool sparse = a.sel != nullptr;
-  const PagedPlan p = paged_attn_plan(rows, a.t_max, a.k_total, sparse);
-  const int per = (a.batch + kThreads - 1) / kThreads, join_per = (a.batch + 255) / 256;
-  const dim3 grid((unsigned)p.n_wgs), block(kThreads);
-  if (sparse)
-    hipLaunchKernelGGL(paged_attn_kernel<true>, grid, block, 0, stream, a, p.row_units, per);
-  else
-    hipLaunchKernelGGL(paged_attn_kernel<false>, grid, block, 0, stream, a, p.row_units, per);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !p.joined) return e;
-  const dim3 join_grid((unsigned)(rows * a.group_size));
-  if (sparse)
-    hipLaunchKernelGGL(paged_join_kernel<true>, join_grid, dim3(256), 0, stream, a, p.row_units, join_per, p.n_wgs);
-  else
-    hipLaunchKernelGGL(paged_join_kernel<false>, join_grid, dim3(256), 0, stream, a, p.row_units, join_per, p.n_wgs);
-  return hipGetLastError();
+  const PagedPlan p = paged_attn_plan((int64_t)a.batch * a.n_kv_heads, a.t_max, a.k_total, a.sel != nullptr);
+  return a.sel ? launch<true>(a, p, stream) : launch<false>(a, p, stream);
 }
 
 }  // namespace sparda

@@ -266,7 +266,7 @@ int sparda_workspace_size(const sparda_shape* shape, int32_t op, int32_t n_q, in
     if (n_q != 1) return fail(SPARDA_ERR_INVALID_ARG, "a paged call has n_q == 1");
     const int64_t rows = (int64_t)shape->batch * shape->n_kv_heads;
     *bytes = op == SPARDA_OP_PAGED_SELECT ? sparda::paged_select_ws(rows, q_pos0 + 1, shape->n_init, shape->n_local)
-                                          : sparda::paged_attn_ws(shape->group_size);
+                                          : sparda::paged_attn_ws(shape->batch, shape->group_size);
   } else {
     return fail(SPARDA_ERR_INVALID_ARG, "unknown op %d", op);
   }
