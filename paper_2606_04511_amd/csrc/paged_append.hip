@@ -33,6 +33,7 @@ template <int L>  // tokens of a window; its stride is 64 with L = 64, else 16
 __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, int slices) {
   constexpr int S = L == 64 ? 64 : 16, kBefore = L - S;
   const int tid = threadIdx.x, c = tid & 7, g = tid >> 3;
+  const Chunks ch = rotary_chunks(a.rope, c);
   const int h = (int)(unit % a.n_kv_heads);
   const int64_t rest = unit / a.n_kv_heads;
   const int b = (int)(rest / slices);
@@ -50,8 +51,6 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
   if (first_end < L) first_end = L;
   const bool windows = a.pg.kc && first_end <= end;
   const int64_t low = windows ? first_end - L : from;  // the first key that a window needs
-  int ca, cb;
-  rotary_chunks(a.rope, c, &ca, &cb);
   for (int rr = g; rr < 64 + kBefore; rr += 32) {
     const int64_t tok = base - kBefore + rr;
     if (tok < low || tok >= end) continue;
@@ -59,52 +58,59 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
     uint4 wa = make_uint4(0u, 0u, 0u, 0u), wb = wa;
     if (tok >= t0) {
       const uint16_t* src = row_of(a.k_new, b, h, tok - t0);
-      wa = ld16(src + 8 * ca);
-      wb = ld16(src + 8 * cb);
+      wa = ld16_nt(src + 8 * ch.a);
+      wb = ld16_nt(src + 8 * ch.b);
       Turns turn;
-      rotary_turns(a.rope, c, tok, 1.f, &turn);
-      rotary_row(a.rope, c, turn, &wa, &wb);
+      rotary_turns(a.rope, c, ch, tok, 1.f, &turn);
+      rotary_row(a.rope, ch, turn, wa, wb);
       if (tok >= base && page >= 0) {
         const uint16_t* vs = row_of(a.v_new, b, h, tok - t0);
-        const uint4 va = ld16(vs + 16 * c), vb = ld16(vs + 16 * c + 8);
+        const uint4 va = ld16_nt(vs + 8 * c), vb = ld16_nt(vs + 8 * c + 64);
         const int64_t at = token_at(a.pg, page, h, tok);
-        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * ca) = wa;
-        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * cb) = wb;
-        *reinterpret_cast<uint4*>(a.pg.v + at + 16 * c) = va;
-        *reinterpret_cast<uint4*>(a.pg.v + at + 16 * c + 8) = vb;
+        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * ch.a) = wa;
+        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * ch.b) = wb;
+        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c) = va;
+        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c + 64) = vb;
       }
     } else if (page >= 0) {
       const uint16_t* src = a.pg.k + token_at(a.pg, page, h, tok);
-      wa = ld16(src + 8 * ca);
-      wb = ld16(src + 8 * cb);
+      wa = ld16(src + 8 * ch.a);
+      wb = ld16(src + 8 * ch.b);
     }
-    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * ca) = wa;
-    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * cb) = wb;
+    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * ch.a) = wa;
+    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * ch.b) = wb;
   }
   if (!windows) return;
   __syncthreads();
-  const int n_win = (int)((end - first_end) / S) + 1, d = tid & 127;
-  for (int w = tid >> 7; w < n_win; w += 2) {
-    const int64_t w_end = first_end + w * S, w_begin = w_end - L;
-    const int32_t page = page_of(a.pg, table, w_begin);
-    if (page < 0 || (L == 32 && page_of(a.pg, table, w_begin + 16) < 0)) continue;
-    const char* rows = lds + (w_begin - (base - kBefore)) * 256 + 2 * d;
-    double sum = 0.0;
+  // a wavefront per window (at most four end in a block), two elements per lane
+  const int n_win = (int)((end - first_end) / S) + 1, w = tid >> 6, d = 2 * (tid & 63);
+  if (w >= n_win) return;
+  const int64_t w_begin = first_end + w * S - L;
+  const int32_t page = page_of(a.pg, table, w_begin);
+  if (page < 0 || (L == 32 && page_of(a.pg, table, w_begin + 16) < 0)) return;
+  const char* rows = lds + (w_begin - (base - kBefore)) * 256 + 2 * d;
+  double s0 = 0.0, s1 = 0.0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      double part = 0.0;
+  for (int r = 0; r < 16; ++r) {
+    double p0 = 0.0, p1 = 0.0;
 #pragma unroll
-      for (int x = 0; x < L / 16; ++x) part += bf16_to_f32(*reinterpret_cast<const uint16_t*>(rows + (r + 16 * x) * 256));
-      sum += part;
+    for (int x = 0; x < L / 16; ++x) {
+      const uint32_t y = *reinterpret_cast<const uint32_t*>(rows + (r + 16 * x) * 256);
+      p0 += bf16lo(y);
+      p1 += bf16hi(y);
     }
-    a.pg.kc[key_at(a.pg, page, a.n_kv_heads, h, w_begin, L == 64 ? 6 : 4) + d] = f64_to_bf16(sum * (1.0 / L));
+    s0 += p0;
+    s1 += p1;
   }
+  *reinterpret_cast<uint32_t*>(a.pg.kc + key_at(a.pg, page, a.n_kv_heads, h, w_begin, L == 64 ? 6 : 4) + d) =
+      f64_to_bf16(s0 * (1.0 / L)) | (uint32_t)f64_to_bf16(s1 * (1.0 / L)) << 16;
 }
 
 // Rows of q (heads [0, Hq)) and f (the Hkv heads behind them) of one token, eight lanes each.
 __device__ void append_turn(const PagedAppendArgs& a, int64_t grp, int64_t n_groups, int heads) {
   if (grp >= n_groups) return;
   const int c = threadIdx.x & 7;
+  const Chunks ch = rotary_chunks(a.rope, c);
   const int hq = a.q.data ? a.n_kv_heads * a.group_size : 0, hf = a.f.data ? a.n_kv_heads : 0;
   const int64_t tokens = (int64_t)a.batch * a.n_max;
   const int64_t tok = grp % tokens;
@@ -113,17 +119,15 @@ __device__ void append_turn(const PagedAppendArgs& a, int64_t grp, int64_t n_gro
   const int64_t t0 = a.t_ctx[b];
   if (j >= new_tokens(a, b, t0)) return;
   Turns turn;
-  rotary_turns(a.rope, c, t0 + j, 1.f, &turn);
-  int ca, cb;
-  rotary_chunks(a.rope, c, &ca, &cb);
+  rotary_turns(a.rope, c, ch, t0 + j, 1.f, &turn);
   for (int h = h0; h < h1; ++h) {
     const bool isq = h < hq;
     const uint16_t* x = isq ? row_of(a.q, b, h, j) : row_of(a.f, b, h - hq, j);
     uint16_t* y = const_cast<uint16_t*>(isq ? row_of(a.q_out, b, h, j) : row_of(a.f_out, b, h - hq, j));
-    uint4 wa = ld16(x + 8 * ca), wb = ld16(x + 8 * cb);
-    rotary_row(a.rope, c, turn, &wa, &wb);
-    *reinterpret_cast<uint4*>(y + 8 * ca) = wa;
-    *reinterpret_cast<uint4*>(y + 8 * cb) = wb;
+    uint4 wa = ld16_nt(x + 8 * ch.a), wb = ld16_nt(x + 8 * ch.b);
+    rotary_row(a.rope, ch, turn, wa, wb);
+    *reinterpret_cast<uint4*>(y + 8 * ch.a) = wa;
+    *reinterpret_cast<uint4*>(y + 8 * ch.b) = wb;
   }
 }
 

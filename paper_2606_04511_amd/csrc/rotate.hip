@@ -6,10 +6,14 @@
 namespace sparda {
 
 namespace {
+__device__ __forceinline__ void st16_nt(void* p, uint4 w) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, w), reinterpret_cast<u32x4_t*>(p));
+}
 
 template <bool kBf16>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t n_groups, int heads) {
   const int c = threadIdx.x & 7;
+  const Chunks ch = rotary_chunks(a.rope, c);
   const int64_t grp = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
   if (grp >= n_groups) return;
   const int64_t tokens = (int64_t)a.batch * a.n_tok;
@@ -17,32 +21,49 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t n_gro
   const int h0 = (int)(grp / tokens) * heads, h1 = min(h0 + heads, a.n_heads);
   const int64_t b = tok / a.n_tok, t = tok % a.n_tok;
   Turns turn;
-  rotary_turns(a.rope, c, a.pos[b * a.pos_ld + t], a.backward ? -1.f : 1.f, &turn);
-  int ca, cb;
-  rotary_chunks(a.rope, c, &ca, &cb);
+  rotary_turns(a.rope, c, ch, a.pos[b * a.pos_ld + t], a.backward ? -1.f : 1.f, &turn);
   const int64_t x0 = b * a.x.ld_batch + t * a.x.ld_token, y0 = b * a.y.ld_batch + t * a.y.ld_token;
-  for (int h = h0; h < h1; ++h) {
+  // the loads of kAhead heads under way (those past the last repeat it)
+  constexpr int kAhead = kBf16 ? 4 : 2;
+  for (int h = h0; h < h1; h += kAhead) {
     if constexpr (kBf16) {
-      const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + x0 + h * a.x.ld_head;
-      uint16_t* y = static_cast<uint16_t*>(a.y.data) + y0 + h * a.y.ld_head;
-      uint4 wa = ld16(x + 8 * ca), wb = ld16(x + 8 * cb);
-      rotary_row(a.rope, c, turn, &wa, &wb);
-      *reinterpret_cast<uint4*>(y + 8 * ca) = wa;
-      *reinterpret_cast<uint4*>(y + 8 * cb) = wb;
-    } else {
-      const float* x = static_cast<const float*>(a.x.data) + x0 + h * a.x.ld_head;
-      float* y = static_cast<float*>(a.y.data) + y0 + h * a.y.ld_head;
-      float v[16];
+      const uint16_t* x = static_cast<const uint16_t*>(a.x.data) + x0;
+      uint16_t* y = static_cast<uint16_t*>(a.y.data) + y0;
+      uint4 wa[kAhead], wb[kAhead];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        *reinterpret_cast<float4*>(v + 4 * i) = *reinterpret_cast<const float4*>(x + 8 * ca + 4 * i);
-        *reinterpret_cast<float4*>(v + 8 + 4 * i) = *reinterpret_cast<const float4*>(x + 8 * cb + 4 * i);
+      for (int e = 0; e < kAhead; ++e) {
+        const uint16_t* src = x + min(h + e, h1 - 1) * a.x.ld_head;
+        wa[e] = ld16_nt(src + 8 * ch.a);
+        wb[e] = ld16_nt(src + 8 * ch.b);
       }
-      rotary_apply(a.rope, c, turn, v);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        *reinterpret_cast<float4*>(y + 8 * ca + 4 * i) = *reinterpret_cast<const float4*>(v + 4 * i);
-        *reinterpret_cast<float4*>(y + 8 * cb + 4 * i) = *reinterpret_cast<const float4*>(v + 8 + 4 * i);
+      for (int e = 0; e < kAhead; ++e) {
+        if (h + e >= h1) break;
+        rotary_row(a.rope, ch, turn, wa[e], wb[e]);
+        uint16_t* dst = y + (h + e) * a.y.ld_head;
+        st16_nt(dst + 8 * ch.a, wa[e]);
+        st16_nt(dst + 8 * ch.b, wb[e]);
+      }
+    } else {
+      const float* x = static_cast<const float*>(a.x.data) + x0;
+      float* y = static_cast<float*>(a.y.data) + y0;
+      uint4 w[kAhead][4];
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        const float* src = x + min(h + e, h1 - 1) * a.x.ld_head;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[e][i] = ld16_nt(src + 8 * (i < 2 ? ch.a : ch.b) + 4 * (i & 1));
+      }
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        if (h + e >= h1) break;
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(v + 4 * i) = w[e][i];
+        rotary_apply(a.rope, ch, turn, v);
+        float* dst = y + (h + e) * a.y.ld_head;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st16_nt(dst + 8 * (i < 2 ? ch.a : ch.b) + 4 * (i & 1), *reinterpret_cast<const uint4*>(v + 4 * i));
       }
     }
   }
@@ -55,6 +76,8 @@ hipError_t launch_rotate(const RotateArgs& a, hipStream_t stream) {
   // heads of a group of lanes: all of them while that leaves about eight wavefronts per SIMD, else fewer
   int64_t heads = tokens * a.n_heads / 65536;
   heads = heads < 1 ? 1 : heads > a.n_heads ? a.n_heads : heads;
+  const int64_t parts = (a.n_heads + heads - 1) / heads;
+  heads = (a.n_heads + parts - 1) / parts;
   const int64_t groups = tokens * ((a.n_heads + heads - 1) / heads);
   const dim3 grid((unsigned)((groups + 31) / 32)), block(256);
   if (a.bf16)
