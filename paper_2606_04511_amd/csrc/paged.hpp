@@ -89,40 +89,32 @@ inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32
   return (size_t)rows * (size_t)paged_select_stride(t_max, n_init, n_local) * sizeof(float);
 }
 
-// How an attention call is cut.  Its work is a line of units of 32 tokens, row by row; every wavefront takes an equal
-// piece of the line, whatever the lengths are, and a piece that holds only a part of a row leaves a partial result.
+// How an attention call is cut.  The work of a row (a sequence's KV head) is counted in units of 32 tokens.  Either every
+// row has n_splits workgroups, which divide it evenly; or (n_splits 0) the rows lie one behind the other on a line, of which
+// every wavefront takes an equal piece, whatever the lengths are.
 constexpr int kPagedWaves = 8;    // wavefronts of a workgroup
 constexpr int kPagedMaxWgs = 256; // one workgroup per CU
+// Units of a row of t tokens, of which a list of k_total blocks (0: no list) may name a part.
+__host__ __device__ inline uint32_t paged_units(int64_t t, int32_t k_total) {
+  if (t <= 0) return 0;
+  if (k_total <= 0) return (uint32_t)((t + 31) >> 5);
+  const int64_t blocks = (t + 63) >> 6;
+  return 2 * (uint32_t)(blocks < k_total ? blocks : k_total);
+}
 struct PagedPlan {
-  int32_t n_wgs;
-  int64_t row_units;  // units of a row (sparse calls; dense ones follow the lengths)
-  bool joined;        // rows may be cut between workgroups, or shared by wavefronts of one that holds other rows
+  int32_t n_wgs, n_splits;
+  bool joined;  // there may be partial results
 };
-inline PagedPlan paged_attn_plan(int64_t rows, int64_t t_max, int32_t k_total, bool sparse) {
-  PagedPlan p;
-  if (sparse) {
-    // up to one row per CU: workgroups per row; a row's units are rounded up to fill their wavefronts evenly (those
-    // past k_total are empty)
-    const int64_t units = 2 * (int64_t)k_total;
-    if (rows <= kPagedMaxWgs) {
-      int64_t s = kPagedMaxWgs / rows;
-      const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
-      s = s < most ? s : most;
-      p.n_wgs = (int32_t)(rows * s);
-      p.row_units = (units + kPagedWaves * s - 1) / (kPagedWaves * s) * (kPagedWaves * s);
-      p.joined = s > 1;
-    } else {
-      p.n_wgs = kPagedMaxWgs;
-      p.row_units = units;
-      p.joined = true;
-    }
-  } else {
-    const int64_t most = (rows * ((t_max + 31) / 32) + kPagedWaves - 1) / kPagedWaves;
-    p.n_wgs = (int32_t)(most < kPagedMaxWgs ? most : kPagedMaxWgs);
-    p.row_units = 0;
-    p.joined = true;
+inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int64_t t_max, int32_t k_total) {
+  const int64_t rows = (int64_t)batch * n_kv_heads, units = paged_units(t_max, k_total);
+  if (rows <= kPagedMaxWgs && (k_total > 0 || batch == 1 || units <= 16)) {
+    int64_t s = kPagedMaxWgs / rows;
+    const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
+    s = units <= 16 ? 1 : s < most ? s : most;
+    return {(int32_t)(rows * s), (int32_t)s, s > 1};
   }
-  return p;
+  const int64_t most = (rows * units + kPagedWaves - 1) / kPagedWaves;
+  return {(int32_t)(most < kPagedMaxWgs ? most : kPagedMaxWgs), 0, true};
 }
 // Two partial results per wavefront, each per head: 128 sums, the maximum and the denominator (4 floats apart).
 constexpr int kPartFloats = 132;

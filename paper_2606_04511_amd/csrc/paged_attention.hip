@@ -1,11 +1,12 @@
 // paged_attention.hip -- attention of every sequence's newest token over the tokens of its listed blocks, or over its whole
 // context, for sequences of different lengths whose K and V lie in pages (paper Sec. 4.1, Eq. 5).
 //
-// The work is a line of units of 32 tokens, row after row (a row is a sequence's KV head with its G query heads), cut into
-// equal pieces, one per wavefront, whatever the lengths are.  The eight wavefronts of a workgroup whose pieces lie in one or
-// two rows divide those rows instead and join their results in LDS.  A wavefront goes over its units once with a running
-// maximum and sum per head.  A row that ends up whole is written; the results of the others go to the workspace and
-// paged_join_kernel joins them.
+// A row is a sequence's KV head with its G query heads; its work is counted in units of 32 tokens.  Where the rows are few
+// and about as long (paged_attn_plan), a row has its own workgroups, which divide it evenly.  Otherwise the rows lie one
+// behind the other on a line, which is cut into equal pieces, one per wavefront, whatever the lengths are; the eight
+// wavefronts of a workgroup whose pieces lie in one or two rows divide those rows instead.  A wavefront goes over its units
+// once with a running maximum and sum per head; those of a workgroup that share a row join their results in LDS.  A row
+// that ends up whole is written; the results of the others go to the workspace and paged_join_kernel joins them.
 //
 // A unit is two slices of 16 tokens, the smallest page.  S^T = K Q^T on the matrix cores with 16 tokens as rows and the
 // heads as columns: K goes through 8 KiB of the wavefront's LDS (whole rows in, fragments of 16 bytes out, swizzled).
@@ -36,9 +37,9 @@ __device__ __forceinline__ int64_t attn_context(const PagedAttnArgs& a, int b) {
   const int64_t t = a.t_ctx[b];
   return t > a.t_max ? a.t_max : t;
 }
-__device__ __forceinline__ uint32_t dense_units(int64_t t) { return t > 0 ? (uint32_t)((t + 31) >> 5) : 0u; }
+__device__ __forceinline__ uint32_t units_of(const PagedAttnArgs& a, int64_t t) { return paged_units(t, a.k_total); }
 
-// Where the sequences of a dense call begin on the line, in units per KV head.  Up to 64 sequences: lane i holds the start
+// Where the sequences begin on the line, in units per KV head.  Up to 64 sequences: lane i holds the start
 // of sequence i, formed by each wavefront on its own.  More: thread i has `per` consecutive sequences and its start is
 // pre[i] in LDS.  Every thread of the workgroup must call it.
 struct Starts {
@@ -49,13 +50,13 @@ __device__ __forceinline__ Starts scan_lengths(const PagedAttnArgs& a, int per, 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t mine = 0;
   if (per == 0) {
-    mine = lane < a.batch ? dense_units(attn_context(a, lane)) : 0u;
+    mine = lane < a.batch ? units_of(a, attn_context(a, lane)) : 0u;
     const uint32_t incl = (uint32_t)wave_incl_scan_dpp((int)mine);
     return {incl - mine, (uint32_t)readlane_i((int)incl, 63)};
   }
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
-    if (b < a.batch) mine += dense_units(attn_context(a, b));
+    if (b < a.batch) mine += units_of(a, attn_context(a, b));
   }
   const uint32_t incl = (uint32_t)wave_incl_scan_dpp((int)mine);
   if (lane == 63) sums[wave] = incl;
@@ -71,8 +72,8 @@ __device__ __forceinline__ Starts scan_lengths(const PagedAttnArgs& a, int per, 
   return {before + incl - mine, total};
 }
 
-// The row that holds unit u (one of the line's) of a dense call.
-__device__ __forceinline__ RowAt dense_row(const PagedAttnArgs& a, int per, const Starts& st, const uint32_t* pre, uint32_t u) {
+// The row that holds unit u of the line.
+__device__ __forceinline__ RowAt line_row(const PagedAttnArgs& a, int per, const Starts& st, const uint32_t* pre, uint32_t u) {
   const int lane = threadIdx.x & 63;
   const uint32_t H = (uint32_t)a.n_kv_heads;
   int b;
@@ -89,7 +90,7 @@ __device__ __forceinline__ RowAt dense_row(const PagedAttnArgs& a, int per, cons
   }
   for (;; ++b) {
     const int64_t t = attn_context(a, b);
-    const uint32_t units = dense_units(t);
+    const uint32_t units = units_of(a, t);
     if (u < at + units * H || b + 1 >= a.batch) {
       const uint32_t h = units > 0 ? (u - at) / units : 0u;
       return {b, (int)h, t, at + h * units, units};
@@ -98,25 +99,19 @@ __device__ __forceinline__ RowAt dense_row(const PagedAttnArgs& a, int per, cons
   }
 }
 // The row behind r that has units.
-__device__ __forceinline__ RowAt next_dense_row(const PagedAttnArgs& a, RowAt r) {
+__device__ __forceinline__ RowAt next_row(const PagedAttnArgs& a, RowAt r) {
   r.u0 += r.units;
   if (++r.h < a.n_kv_heads) return r;
   r.h = 0;
   while (++r.b < a.batch) {
     r.t = attn_context(a, r.b);
-    r.units = dense_units(r.t);
+    r.units = units_of(a, r.t);
     if (r.units > 0) return r;
   }
   r.units = 0;  // past the line
   return r;
 }
-__device__ __forceinline__ RowAt sparse_row(const PagedAttnArgs& a, uint32_t row_units, uint32_t u) {
-  const uint32_t row = u / row_units;
-  const int b = (int)(row / (uint32_t)a.n_kv_heads), h = (int)(row % (uint32_t)a.n_kv_heads);
-  return {b, h, attn_context(a, b), row * row_units, row_units};
-}
-
-// The workspace: whether the wavefronts of workgroup i share their rows; where sequence b begins on the line (dense calls);
+// The workspace: whether the wavefronts of workgroup i share their rows; where sequence b begins on the line;
 // the partial results, two per wavefront.
 __device__ __forceinline__ int32_t* shared_flags(const PagedAttnArgs& a) { return reinterpret_cast<int32_t*>(a.ws); }
 __device__ __forceinline__ uint32_t* line_starts(const PagedAttnArgs& a) {
@@ -138,15 +133,17 @@ struct Running {
   float m, l;
 };
 
-// The wavefront's units [u0, u1) of row r (counted within the row).
+// The wavefront's units [u0, u1) of row r (counted within the row; those of a list are the blocks that it names, in its
+// order, each once).  list: 64 block indices of the wavefront's own LDS.
 template <bool kSparse>
-__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, int u0, int u1, char* kbuf, Running* run) {
+__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, int u0, int u1, char* kbuf, int16_t* list,
+                                       Running* run) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) run->acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   run->m = -INFINITY;
   run->l = 0.f;
-  if (r.t <= 0) return;
+  if (u0 >= u1) return;
   const int64_t row = (int64_t)r.b * a.n_kv_heads + r.h;
   const int32_t* table = a.pg.table + r.b * a.pg.table_ld;
   bf16x8 qf[4];
@@ -155,41 +152,9 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, i
 #pragma unroll
     for (int s = 0; s < 4; ++s) qf[s] = as_bf16x8(c < a.group_size ? ld16(q + 32 * s) : make_uint4(0u, 0u, 0u, 0u));
   }
-  int cnt = 0;
-  bool ascending = true;
-  const int16_t* sel = nullptr;
-  if constexpr (kSparse) {
-    sel = a.sel + row * a.k_total;
-    cnt = a.cnt[row];
-    cnt = cnt < 0 ? 0 : cnt > a.k_total ? a.k_total : cnt;
-    // a list that ascends strictly names no block twice
-    const int last = min(cnt, (u1 + 1) >> 1);
-    for (int i0 = 0; i0 < last; i0 += 64) {
-      const int i = i0 + lane;
-      if (__ballot(i > 0 && i < last && sel[min(i, last - 1)] <= sel[max(min(i, last - 1) - 1, 0)]) != 0ull) ascending = false;
-    }
-  }
-  for (int hb = u0; hb < u1; hb += 32) {
-    // lane i: slice i of the next 32 units; lim: its tokens
-    int64_t tok = 0, off = 0;
-    int lim = 0;
-    const int u = hb + (lane >> 1);
-    if constexpr (kSparse) {
-      const int e = u >> 1;
-      if (u < u1 && e < cnt) {
-        const int blk = sel[e];
-        tok = (int64_t)blk * 64 + (u & 1) * 32 + (lane & 1) * 16;
-        if (blk >= 0 && tok < r.t) {
-          lim = (int)min(r.t - tok, (int64_t)16);
-          if (!ascending)
-            for (int x = 0; x < e; ++x)
-              if (sel[x] == blk) lim = 0;
-        }
-      }
-    } else {
-      tok = (int64_t)u * 32 + (lane & 1) * 16;
-      if (u < u1 && tok < r.t) lim = (int)min(r.t - tok, (int64_t)16);
-    }
+  // Up to 32 units: lane i has slice i of them, from token tok on, lim tokens of it (0: none).
+  auto chunk = [&](int64_t tok, int lim) {
+    int64_t off = 0;
     if (lim > 0) {
       const int32_t page = page_of(a.pg, table, tok);
       if (page >= 0)
@@ -204,7 +169,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, i
     }
     const uint64_t slices = __ballot(lim > 0);
     uint64_t todo = (slices | slices >> 1) & 0x5555555555555555ull;
-    if (todo == 0ull) continue;
+    if (todo == 0ull) return;
     const int off_lo = (int)(uint32_t)off, off_hi = (int)(off >> 32);
     auto slice_at = [&](int i) {
       return (int64_t)(((uint64_t)(uint32_t)readlane_i(off_hi, i) << 32) | (uint32_t)readlane_i(off_lo, i));
@@ -313,6 +278,46 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, i
       i = next;
     }
     unit(i, 0, std::false_type{});
+  };
+  if constexpr (!kSparse) {
+    for (int hb = u0; hb < u1; hb += 32) {
+      const int u = hb + (lane >> 1);
+      const int64_t tok = (int64_t)u * 32 + (lane & 1) * 16, left = r.t - tok;
+      chunk(tok, u < u1 && left > 0 ? (int)(left < 16 ? left : 16) : 0);
+    }
+  } else {
+    const int16_t* sel = a.sel + row * a.k_total;
+    int cnt = a.cnt[row];
+    cnt = cnt > a.k_total ? a.k_total : cnt;
+    bool ascending = true;  // so far: a list that ascends strictly names no block twice
+    int before = 0;         // blocks that the entries before i0 name
+    for (int i0 = 0; i0 < cnt && 2 * before < u1; i0 += 64) {
+      const int i = i0 + lane;
+      const int blk = i < cnt ? sel[i] : -1;
+      bool in = blk >= 0 && (int64_t)blk * 64 < r.t;
+      if (__ballot(i > 0 && i < cnt && sel[max(min(i, cnt - 1) - 1, 0)] >= blk) != 0ull) ascending = false;
+      if (!ascending)
+        for (int x = 0; x < i && in; ++x)
+          if (sel[x] == blk) in = false;
+      const uint64_t named = __ballot(in);
+      const int n = (int)__popcll(named);
+      if (2 * (before + n) > u0) {
+        if (in) list[mbcnt64(named)] = (int16_t)blk;
+        wave_lds_sync();
+        const int first = max((u0 >> 1) - before, 0), last = min(((u1 + 1) >> 1) - before, n);
+        for (int c0 = first; c0 < last; c0 += 16) {
+          const int e = c0 + (lane >> 2), u = 2 * (before + e) + ((lane >> 1) & 1);
+          int64_t tok = 0, left = 0;
+          if (e < last && u >= u0 && u < u1) {
+            tok = (int64_t)list[e] * 64 + (lane & 3) * 16;
+            left = r.t - tok;
+          }
+          chunk(tok, left > 0 ? (int)(left < 16 ? left : 16) : 0);
+        }
+        wave_lds_sync();
+      }
+      before += n;
+    }
   }
   run->l += __shfl_xor(run->l, 16, 64);
   run->l += __shfl_xor(run->l, 32, 64);
@@ -354,20 +359,86 @@ __device__ __forceinline__ float join_weight(float m, float top) {
   return m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);  // (both -inf: the part is empty, its sums are zero)
 }
 
-template <bool kSparse>
-__global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a, uint32_t row_units, int per) {
-  __shared__ __align__(16) char kbuf[kPagedWaves][32 * 256];
-  __shared__ uint32_t pre[kSparse ? 1 : kThreads], sums[kPagedWaves];
-  __shared__ float stat[kPagedWaves][16][2];
+// The wavefronts' results of a workgroup that share row r, joined (a head's 128 sums of a wavefront in its K buffer, 16
+// bytes at a time; piece x of head c lies at x ^ 2 c, free of bank conflicts): to the output, or to partial result `slot`.
+// Every thread of the workgroup must call it.
+__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const RowAt& r, const Running& run, char (*kbuf)[32 * 256],
+                                           float (*stat)[16][2], bool whole, int64_t slot) {
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  char* mine = kbuf[wave] + c * 512;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x) ^ (2 * c))) = f32x4{run.acc[0][x], run.acc[1][x], run.acc[2][x], run.acc[3][x]};
+    *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x + 1) ^ (2 * c))) = f32x4{run.acc[4][x], run.acc[5][x], run.acc[6][x], run.acc[7][x]};
+  }
+  if (g == 0) {
+    stat[wave][c][0] = run.m;
+    stat[wave][c][1] = run.l;
+  }
+  __syncthreads();
+  for (int i = tid; i < a.group_size * 32; i += kThreads) {
+    const int head = i >> 5, x = i & 31;
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, stat[w][head][0]);
+    f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kPagedWaves; ++w) {
+      const float f = join_weight(stat[w][head][0], top);
+      l = fmaf(f, stat[w][head][1], l);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(kbuf[w] + head * 512 + 16 * (x ^ (2 * head)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, y[e], sum[e]);
+    }
+    if (whole) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      uint16_t* o = a.o + (((int64_t)r.b * a.n_kv_heads + r.h) * a.group_size + head) * kHeadDim + 4 * x;
+      *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
+    } else {
+      float* dst = partial(a, slot, head);
+      *reinterpret_cast<f32x4*>(dst + 4 * x) = sum;
+      if (x == 0) *reinterpret_cast<float2*>(dst + 128) = make_float2(top, l);
+    }
+  }
+}
+
+// Wavefront w's share of n units.
+__device__ __forceinline__ void share_of(uint32_t n, int w, int parts, uint32_t* v0, uint32_t* v1) {
+  const uint32_t each = (n + parts - 1) / parts;
+  *v0 = w * each < n ? w * each : n;
+  *v1 = *v0 + each < n ? *v0 + each : n;
+}
+
+// n_splits > 0: n_splits workgroups per row; 0: the line.
+template <bool kSparse>
+__global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a, int n_splits, int per) {
+  __shared__ __align__(16) char kbuf[kPagedWaves][32 * 256];
+  __shared__ uint32_t pre[kThreads], sums[kPagedWaves];
+  __shared__ float stat[kPagedWaves][16][2];
+  __shared__ int16_t lists[kPagedWaves][kSparse ? 64 : 1];
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Running run;
+  RowAt r, second;
+  uint32_t w0, w1, piece = 0;
   Starts st = {0u, 0u};
-  uint32_t total;
-  if constexpr (kSparse) {
-    total = (uint32_t)(a.batch * a.n_kv_heads) * row_units;
+  if (n_splits > 0) {
+    const uint32_t row = blockIdx.x / (uint32_t)n_splits, split = blockIdx.x % (uint32_t)n_splits;
+    r.b = (int)(row / (uint32_t)a.n_kv_heads);
+    r.h = (int)(row % (uint32_t)a.n_kv_heads);
+    r.t = attn_context(a, r.b);
+    r.u0 = 0;
+    r.units = units_of(a, r.t);
+    // the row's shares are those of its n_splits * 8 wavefronts
+    const uint32_t each = (r.units + n_splits * kPagedWaves - 1) / (n_splits * kPagedWaves) * kPagedWaves;
+    w0 = split * each < r.units ? split * each : r.units;
+    w1 = w0 + each < r.units ? w0 + each : r.units;
+    second = r;
   } else {
     st = scan_lengths(a, per, pre, sums);
-    total = st.total * (uint32_t)a.n_kv_heads;
+    const uint32_t total = st.total * (uint32_t)a.n_kv_heads;
     if (blockIdx.x == 0) {  // for the join
       uint32_t* starts = line_starts(a);
       const int n = per == 0 ? 1 : per;
@@ -376,7 +447,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
         const int b = tid * n + i;
         if (b >= a.batch || (per == 0 && wave > 0)) break;
         starts[b] = at;
-        at += dense_units(attn_context(a, b));
+        at += units_of(a, attn_context(a, b));
       }
       if (tid == 0) starts[a.batch] = st.total;
     }
@@ -386,125 +457,57 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
         uint4* o = reinterpret_cast<uint4*>(a.o + (int64_t)b * a.n_kv_heads * a.group_size * kHeadDim);
         for (int i = tid; i < a.n_kv_heads * a.group_size * (kHeadDim / 8); i += kThreads) o[i] = make_uint4(0u, 0u, 0u, 0u);
       }
-  }
-  const uint32_t piece = line_piece(total, gridDim.x);
-  const uint32_t w0 = blockIdx.x * kPagedWaves * piece;
-  if (w0 >= total) return;
-  const uint32_t w1 = total - w0 < kPagedWaves * piece ? total : w0 + kPagedWaves * piece;
-  auto row_at = [&](uint32_t u) {
-    if constexpr (kSparse)
-      return sparse_row(a, row_units, u);
-    else
-      return dense_row(a, per, st, pre, u);
-  };
-  auto next_row = [&](const RowAt& r) {
-    if constexpr (kSparse)
-      return sparse_row(a, row_units, r.end());
-    else
-      return next_dense_row(a, r);
-  };
-  Running run;
-  RowAt r = row_at(w0);
-  RowAt second = r;
-  if (r.end() < w1) second = next_row(r);
-  const bool share = second.end() >= w1;
-  if (tid == 0) shared_flags(a)[blockIdx.x] = share ? 1 : 0;
-  if (share) {
-    // one row or two: the wavefronts divide each, and their results join in LDS (a head's 128 sums of a wavefront in its
-    // K buffer, 16 bytes at a time; piece x of head c lies at x ^ 2 c, free of bank conflicts)
-    for (uint32_t u = w0;;) {
-      const uint32_t end = r.end() < w1 ? r.end() : w1, n = end - u, each = (n + kPagedWaves - 1) / kPagedWaves;
-      const uint32_t v0 = wave * each < n ? wave * each : n, v1 = v0 + each < n ? v0 + each : n;
-      attend<kSparse>(a, r, (int)(u - r.u0 + v0), (int)(u - r.u0 + v1), kbuf[wave], &run);
-      char* mine = kbuf[wave] + c * 512;
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x) ^ (2 * c))) = f32x4{run.acc[0][x], run.acc[1][x], run.acc[2][x], run.acc[3][x]};
-        *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x + 1) ^ (2 * c))) = f32x4{run.acc[4][x], run.acc[5][x], run.acc[6][x], run.acc[7][x]};
+    piece = line_piece(total, gridDim.x);
+    w0 = blockIdx.x * kPagedWaves * piece;
+    if (w0 >= total) return;
+    w1 = total - w0 < kPagedWaves * piece ? total : w0 + kPagedWaves * piece;
+    r = line_row(a, per, st, pre, w0);
+    second = r.end() < w1 ? next_row(a, r) : r;
+    const bool share = second.end() >= w1;
+    if (tid == 0) shared_flags(a)[blockIdx.x] = share ? 1 : 0;
+    if (!share) {  // several short rows
+      const uint32_t p0 = w0 + wave * piece, p1 = p0 + piece < w1 ? p0 + piece : w1;
+      if (p0 >= p1) return;
+      r = line_row(a, per, st, pre, p0);
+      for (uint32_t u = p0;;) {
+        const uint32_t end = r.end() < p1 ? r.end() : p1;
+        attend<kSparse>(a, r, (int)(u - r.u0), (int)(end - r.u0), kbuf[wave], lists[wave], &run);
+        if (u == r.u0 && end == r.end())
+          write_row(a, r, run);
+        else if (c < a.group_size)
+          write_partial(partial(a, ((int64_t)blockIdx.x * kPagedWaves + wave) * 2 + (u == p0 ? 0 : 1), c), run);
+        u = end;
+        if (u >= p1) return;
+        r = next_row(a, r);
       }
-      if (g == 0) {
-        stat[wave][c][0] = run.m;
-        stat[wave][c][1] = run.l;
-      }
-      __syncthreads();
-      const bool whole = u == r.u0 && end == r.end();
-      for (int i = tid; i < a.group_size * 32; i += kThreads) {
-        const int head = i >> 5, x = i & 31;
-        float top = -INFINITY, f[kPagedWaves], l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) top = fmaxf(top, stat[w][head][0]);
-        f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kPagedWaves; ++w) {
-          f[w] = join_weight(stat[w][head][0], top);
-          l = fmaf(f[w], stat[w][head][1], l);
-          const f32x4 y = *reinterpret_cast<const f32x4*>(kbuf[w] + head * 512 + 16 * (x ^ (2 * head)));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] = fmaf(f[w], y[e], sum[e]);
-        }
-        if (whole) {
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          uint16_t* o = a.o + (((int64_t)r.b * a.n_kv_heads + r.h) * a.group_size + head) * kHeadDim + 4 * x;
-          *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv));
-        } else {
-          float* dst = partial(a, (int64_t)blockIdx.x * kPagedWaves * 2 + (u == w0 ? 0 : 1), head);
-          *reinterpret_cast<f32x4*>(dst + 4 * x) = sum;
-          if (x == 0) *reinterpret_cast<float2*>(dst + 128) = make_float2(top, l);
-        }
-      }
-      u = end;
-      if (u >= w1) return;
-      r = second;
-      __syncthreads();  // the results have been read
     }
   }
-  const uint32_t p0 = w0 + wave * piece, p1 = p0 + piece < w1 ? p0 + piece : w1;
-  if (p0 >= p1) return;
-  r = row_at(p0);
-  for (uint32_t u = p0;;) {
-    const uint32_t end = r.end() < p1 ? r.end() : p1;
-    attend<kSparse>(a, r, (int)(u - r.u0), (int)(end - r.u0), kbuf[wave], &run);
-    if (u == r.u0 && end == r.end())
-      write_row(a, r, run);
-    else if (c < a.group_size)
-      write_partial(partial(a, ((int64_t)blockIdx.x * kPagedWaves + wave) * 2 + (u == p0 ? 0 : 1), c), run);
+  // one row or two, each divided by the wavefronts
+  for (uint32_t u = w0;;) {
+    const uint32_t end = r.end() < w1 ? r.end() : w1;
+    uint32_t v0, v1;
+    share_of(end - u, wave, kPagedWaves, &v0, &v1);
+    attend<kSparse>(a, r, (int)(u - r.u0 + v0), (int)(u - r.u0 + v1), kbuf[wave], lists[wave], &run);
+    const bool whole = n_splits > 0 ? n_splits == 1 : u == r.u0 && end == r.end();
+    join_waves(a, r, run, kbuf, stat, whole, (int64_t)blockIdx.x * kPagedWaves * 2 + (u == w0 ? 0 : 1));
     u = end;
-    if (u >= p1) return;
-    r = next_row(r);
+    if (u >= w1) return;
+    r = second;
+    __syncthreads();  // the results have been read
   }
 }
 
-// Joins the partial results of a row's head, in the order of the line: kWaves wavefronts per (row, head), two elements per
-// lane, eight results requested at once.
-template <bool kSparse, int kWaves>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, uint32_t row_units, int n_wgs, int n_pairs) {
-  __shared__ float acc[4][128], stat[4][2];
+// Joins the partial results of a row's head, in their order: kWaves wavefronts per (row, head), two elements per lane, eight
+// results requested at once.
+template <int kWaves>
+__global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void paged_join_kernel(PagedAttnArgs a, int n_splits, int n_wgs, int n_pairs) {
+  constexpr int kPerWg = kWaves == 1 ? 4 : 1;  // (row, head) pairs of a workgroup
+  __shared__ float acc[kWaves][128], stat[kWaves][2];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave % kWaves;
-  const int pair = (int)blockIdx.x * (4 / kWaves) + wave / kWaves;
+  const int pair = (int)blockIdx.x * kPerWg + (kWaves == 1 ? wave : 0);
   if (pair >= n_pairs) return;
   const int row = pair / a.group_size, head = pair % a.group_size;
-  uint32_t total, u0, units;
-  if constexpr (kSparse) {
-    u0 = (uint32_t)row * row_units;
-    units = row_units;
-    total = (uint32_t)(a.batch * a.n_kv_heads) * row_units;
-  } else {
-    const int b = row / a.n_kv_heads;
-    const uint32_t* starts = line_starts(a);
-    const uint32_t at = starts[b], next = starts[b + 1];
-    units = next - at;
-    u0 = at * (uint32_t)a.n_kv_heads + (uint32_t)(row % a.n_kv_heads) * units;
-    total = starts[a.batch] * (uint32_t)a.n_kv_heads;
-    if (units == 0) return;
-  }
-  const uint32_t end = u0 + units, piece = line_piece(total, n_wgs), wg = piece * kPagedWaves;
-  const int g0 = (int)(u0 / wg), g1 = (int)((end - 1) / wg);
-  const int32_t* flags = shared_flags(a);
-  if (g0 == g1) {  // written by its workgroup, or by one wavefront?
-    if (flags[g0] != 0 || u0 / piece == (end - 1) / piece) return;
-  }
   float m = -INFINITY, l = 0.f, s0 = 0.f, s1 = 0.f;
   auto take8 = [&](auto slot_of, uint32_t valid) {  // results e whose bit is set
     float pm[8], pl[8], x0[8], x1[8], top = m;
@@ -537,21 +540,38 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, uint32
     }
     m = top;
   };
-  for (int x0 = g0 + 8 * part; x0 <= g1; x0 += 8 * kWaves) {
-    const int flag = lane < 8 && x0 + lane <= g1 ? flags[x0 + lane] : -1;
-    const uint32_t joined = (uint32_t)__ballot(flag == 1), apart = (uint32_t)__ballot(flag == 0);
-    // slot 0 holds the result that begins where the piece does
-    if (joined)
-      take8([&](int e) { return (int64_t)(x0 + e) * (kPagedWaves * 2) + ((uint32_t)(x0 + e) * wg >= u0 ? 0 : 1); }, joined);
-    for (uint32_t todo = apart; todo != 0u; todo &= todo - 1u) {
-      const int x = x0 + __builtin_ctz(todo);
-      uint32_t in = 0;
+  if (n_splits > 0) {
+    for (int x = 8 * part; x < n_splits; x += 8 * kWaves)
+      take8([&](int e) { return ((int64_t)row * n_splits + x + e) * (kPagedWaves * 2); },
+            n_splits - x >= 8 ? 0xffu : (1u << (n_splits - x)) - 1u);
+  } else {
+    const int b = row / a.n_kv_heads;
+    const uint32_t* starts = line_starts(a);
+    const uint32_t at = starts[b], units = starts[b + 1] - at, total = starts[a.batch] * (uint32_t)a.n_kv_heads;
+    if (units == 0) return;
+    const uint32_t u0 = at * (uint32_t)a.n_kv_heads + (uint32_t)(row % a.n_kv_heads) * units, end = u0 + units;
+    const uint32_t piece = line_piece(total, n_wgs), wg = piece * kPagedWaves;
+    const int g0 = (int)(u0 / wg), g1 = (int)((end - 1) / wg);
+    const int32_t* flags = shared_flags(a);
+    if (g0 == g1) {  // written by its workgroup, or by one wavefront?
+      if (flags[g0] != 0 || u0 / piece == (end - 1) / piece) return;
+    }
+    for (int x0 = g0 + 8 * part; x0 <= g1; x0 += 8 * kWaves) {
+      const int flag = lane < 8 && x0 + lane <= g1 ? flags[x0 + lane] : -1;
+      const uint32_t joined = (uint32_t)__ballot(flag == 1), apart = (uint32_t)__ballot(flag == 0);
+      // slot 0 holds the result that begins where the piece does
+      if (joined)
+        take8([&](int e) { return (int64_t)(x0 + e) * (kPagedWaves * 2) + ((uint32_t)(x0 + e) * wg >= u0 ? 0 : 1); }, joined);
+      for (uint32_t todo = apart; todo != 0u; todo &= todo - 1u) {
+        const int x = x0 + __builtin_ctz(todo);
+        uint32_t in = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t p0 = (uint32_t)x * wg + e * piece;
-        if (p0 < end && p0 + piece > u0) in |= 1u << e;
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t p0 = (uint32_t)x * wg + e * piece;
+          if (p0 < end && p0 + piece > u0) in |= 1u << e;
+        }
+        take8([&](int e) { return ((int64_t)x * kPagedWaves + e) * 2 + ((uint32_t)x * wg + e * piece >= u0 ? 0 : 1); }, in);
       }
-      take8([&](int e) { return ((int64_t)x * kPagedWaves + e) * 2 + ((uint32_t)x * wg + e * piece >= u0 ? 0 : 1); }, in);
     }
   }
   uint32_t* out = reinterpret_cast<uint32_t*>(a.o + ((int64_t)row * a.group_size + head) * kHeadDim);
@@ -568,9 +588,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, uint32
     if (wave != 0) return;
     float top = -INFINITY, y0 = 0.f, y1 = 0.f, den = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w][0]);
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][0]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       const float f = join_weight(stat[w][0], top);
       const float2 x = *reinterpret_cast<const float2*>(&acc[w][2 * lane]);
       y0 = fmaf(f, x.x, y0);
@@ -582,26 +602,29 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, uint32
   }
 }
 
-template <bool kSparse>
-hipError_t launch(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t stream) {
-  const int per = a.batch <= 64 ? 0 : (a.batch + kThreads - 1) / kThreads;
-  hipLaunchKernelGGL(paged_attn_kernel<kSparse>, dim3((unsigned)p.n_wgs), dim3(kThreads), 0, stream, a, (uint32_t)p.row_units, per);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !p.joined) return e;
-  // rows are cut into about n_wgs / rows + 1 results: four wavefronts per head where those are more than eight
-  const int rows = a.batch * a.n_kv_heads, pairs = rows * a.group_size;
-  if (rows * 8 < p.n_wgs)
-    hipLaunchKernelGGL((paged_join_kernel<kSparse, 4>), dim3((unsigned)pairs), dim3(256), 0, stream, a, (uint32_t)p.row_units, p.n_wgs, pairs);
-  else
-    hipLaunchKernelGGL((paged_join_kernel<kSparse, 1>), dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, a, (uint32_t)p.row_units, p.n_wgs, pairs);
-  return hipGetLastError();
-}
-
 }  // namespace
 
-hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t stream) {
-  const PagedPlan p = paged_attn_plan((int64_t)a.batch * a.n_kv_heads, a.t_max, a.k_total, a.sel != nullptr);
-  return a.sel ? launch<true>(a, p, stream) : launch<false>(a, p, stream);
+hipError_t launch_paged_attn(const PagedAttnArgs& args, hipStream_t stream) {
+  PagedAttnArgs a = args;
+  if (!a.sel) a.k_total = 0;
+  const PagedPlan p = paged_attn_plan(a.batch, a.n_kv_heads, a.t_max, a.k_total);
+  const int per = a.batch <= 64 ? 0 : (a.batch + kThreads - 1) / kThreads;
+  const dim3 grid((unsigned)p.n_wgs), block(kThreads);
+  if (a.sel)
+    hipLaunchKernelGGL(paged_attn_kernel<true>, grid, block, 0, stream, a, p.n_splits, per);
+  else
+    hipLaunchKernelGGL(paged_attn_kernel<false>, grid, block, 0, stream, a, p.n_splits, per);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.joined) return e;
+  // a row has about n_wgs / rows + 1 results: as many wavefronts as take them eight at a time, up to sixteen
+  const int rows = a.batch * a.n_kv_heads, pairs = rows * a.group_size, results = p.n_wgs / rows;
+  if (results > 64)
+    hipLaunchKernelGGL(paged_join_kernel<16>, dim3((unsigned)pairs), dim3(1024), 0, stream, a, p.n_splits, p.n_wgs, pairs);
+  else if (results > 8)
+    hipLaunchKernelGGL(paged_join_kernel<4>, dim3((unsigned)pairs), dim3(256), 0, stream, a, p.n_splits, p.n_wgs, pairs);
+  else
+    hipLaunchKernelGGL(paged_join_kernel<1>, dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, a, p.n_splits, p.n_wgs, pairs);
+  return hipGetLastError();
 }
 
 }  // namespace sparda

@@ -413,6 +413,11 @@ SPARSE = [
     ((9000, 8000), 1, 12, 140, 16, "twice"),
     (tuple(range(10, 3000, 73)), 8, 2, 13, 64, "mixed"),       # 328 rows: more than workgroups
     ((600,) * 300, 1, 5, 5, 256, "sorted"),
+    ((5000, 0, 70, -1, 640), 2, 4, 40, 64, "sorted"),          # rows of several workgroups, some without tokens
+    ((5000, 0, 70, -1, 640), 2, 4, 40, 16, "mixed"),
+    (tuple(range(1, 2000, 29)) + (0, -9), 4, 1, 64, 32, "sorted"),  # lists longer than most contexts
+    (tuple(range(1, 2000, 29)) + (0, -9), 4, 1, 70, 32, "twice"),
+    ((100000,), 1, 2, 1000, 64, "sorted"),
 ]
 
 
