@@ -90,8 +90,17 @@ inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32
 }
 
 // How an attention call is cut.  The work of a row (a sequence's KV head) is counted in units of 32 tokens.  Either every
-// row has n_splits workgroups, which divide it evenly; or (n_splits 0) the rows lie one behind the other on a line, of which
-// every wavefront takes an equal piece, whatever the lengths are.
+// row has n_splits workgroups, which divide it evenly; or (n_splits 0) the rows lie one behind the other on a line, which is
+// cut into equal pieces whatever the lengths are, at the price of a scan over the lengths and a second launch (about 7 us).
+//
+// The host knows the longest context only.  A workgroup alone reads about 50 GB/s, 0.33 us per unit: up to 64 units of the
+// longest row per workgroup, workgroups per row cost at most 20 us where all other rows are short, and are faster where
+// they are not (us, contexts between half of t and t; line and workgroups per row): 32 rows of t = 500 12.1 and 8.1; 256
+// rows of 1000 24 and 19; 512 rows of 1000 with 4 heads 42 and 35, with 16 heads 55 and 37; 1600 rows of 1000 113 and 101;
+// but 320 rows of 2000 46 and 49, the second round being short.  Rows of the same length need no line: those of one
+// sequence, or of lists that are shorter than the contexts, while they fill at most one round of workgroups (256 rows of 64
+// blocks 85 and 82; 320 rows 107 and 122).  Many rows of a few units go to single wavefronts on the line (3200 rows of 100
+// tokens 41 and 54 us; with 16 heads, whose partial results weigh more, 66 and 59).
 constexpr int kPagedWaves = 8;    // wavefronts of a workgroup
 constexpr int kPagedMaxWgs = 256; // one workgroup per CU
 // Units of a row of t tokens, of which a list of k_total blocks (0: no list) may name a part.
@@ -105,16 +114,16 @@ struct PagedPlan {
   int32_t n_wgs, n_splits;
   bool joined;  // there may be partial results
 };
-inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int64_t t_max, int32_t k_total) {
+inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int32_t group_size, int64_t t_max, int32_t k_total) {
   const int64_t rows = (int64_t)batch * n_kv_heads, units = paged_units(t_max, k_total);
-  if (rows <= kPagedMaxWgs && (k_total > 0 || batch == 1 || units <= 16)) {
-    int64_t s = kPagedMaxWgs / rows;
-    const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
-    s = units <= 16 ? 1 : s < most ? s : most;
-    return {(int32_t)(rows * s), (int32_t)s, s > 1};
-  }
-  const int64_t most = (rows * units + kPagedWaves - 1) / kPagedWaves;
-  return {(int32_t)(most < kPagedMaxWgs ? most : kPagedMaxWgs), 0, true};
+  int64_t s = rows <= kPagedMaxWgs && units > 16 ? kPagedMaxWgs / rows : 1;
+  const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
+  s = s < most ? s : most;
+  const bool alike = rows <= kPagedMaxWgs && (batch == 1 || k_total > 0);
+  const bool tiny = rows > 1024 && units <= 8 && group_size <= 8;
+  if (alike || (units <= 64 * s && !tiny)) return {(int32_t)(rows * s), (int32_t)s, s > 1};
+  const int64_t wgs = (rows * units + kPagedWaves - 1) / kPagedWaves;
+  return {(int32_t)(wgs < kPagedMaxWgs ? wgs : kPagedMaxWgs), 0, true};
 }
 // Two partial results per wavefront, each per head: 128 sums, the maximum and the denominator (4 floats apart).
 constexpr int kPartFloats = 132;

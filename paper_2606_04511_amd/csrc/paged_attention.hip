@@ -3,8 +3,8 @@
 //
 // A row is a sequence's KV head with its G query heads; its work is counted in units of 32 tokens.  Where the rows are few
 // and about as long (paged_attn_plan), a row has its own workgroups, which divide it evenly.  Otherwise the rows lie one
-// behind the other on a line, which is cut into equal pieces, one per wavefront, whatever the lengths are; the eight
-// wavefronts of a workgroup whose pieces lie in one or two rows divide those rows instead.  A wavefront goes over its units
+// behind the other on a line, which is cut into equal pieces, one per wavefront, whatever the lengths are; where a workgroup's
+// piece holds long rows, its wavefronts divide each of them instead.  A wavefront goes over its units
 // once with a running maximum and sum per head; those of a workgroup that share a row join their results in LDS.  A row
 // that ends up whole is written; the results of the others go to the workspace and paged_join_kernel joins them.
 //
@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Running run;
-  RowAt r, second;
+  RowAt r;
   uint32_t w0, w1, piece = 0;
   Starts st = {0u, 0u};
   if (n_splits > 0) {
@@ -435,7 +435,6 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
     const uint32_t each = (r.units + n_splits * kPagedWaves - 1) / (n_splits * kPagedWaves) * kPagedWaves;
     w0 = split * each < r.units ? split * each : r.units;
     w1 = w0 + each < r.units ? w0 + each : r.units;
-    second = r;
   } else {
     st = scan_lengths(a, per, pre, sums);
     const uint32_t total = st.total * (uint32_t)a.n_kv_heads;
@@ -462,8 +461,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
     if (w0 >= total) return;
     w1 = total - w0 < kPagedWaves * piece ? total : w0 + kPagedWaves * piece;
     r = line_row(a, per, st, pre, w0);
-    second = r.end() < w1 ? next_row(a, r) : r;
-    const bool share = second.end() >= w1;
+    const RowAt last = r.end() < w1 ? line_row(a, per, st, pre, w1 - 1) : r;
+    const uint32_t n_rows = (uint32_t)(last.b - r.b) * (uint32_t)a.n_kv_heads + (uint32_t)(last.h - r.h) + 1;
+    const bool share = n_rows <= 2 || (w1 - w0) / 16 >= n_rows;
     if (tid == 0) shared_flags(a)[blockIdx.x] = share ? 1 : 0;
     if (!share) {  // several short rows
       const uint32_t p0 = w0 + wave * piece, p1 = p0 + piece < w1 ? p0 + piece : w1;
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
       }
     }
   }
-  // one row or two, each divided by the wavefronts
+  // every row divided by the wavefronts
   for (uint32_t u = w0;;) {
     const uint32_t end = r.end() < w1 ? r.end() : w1;
     uint32_t v0, v1;
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
     join_waves(a, r, run, kbuf, stat, whole, (int64_t)blockIdx.x * kPagedWaves * 2 + (u == w0 ? 0 : 1));
     u = end;
     if (u >= w1) return;
-    r = second;
+    r = next_row(a, r);
     __syncthreads();  // the results have been read
   }
 }
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void paged_join_kernel(P
 hipError_t launch_paged_attn(const PagedAttnArgs& args, hipStream_t stream) {
   PagedAttnArgs a = args;
   if (!a.sel) a.k_total = 0;
-  const PagedPlan p = paged_attn_plan(a.batch, a.n_kv_heads, a.t_max, a.k_total);
+  const PagedPlan p = paged_attn_plan(a.batch, a.n_kv_heads, a.group_size, a.t_max, a.k_total);
   const int per = a.batch <= 64 ? 0 : (a.batch + kThreads - 1) / kThreads;
   const dim3 grid((unsigned)p.n_wgs), block(kThreads);
   if (a.sel)
