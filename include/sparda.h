@@ -588,7 +588,8 @@ int sparda_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double fact
  *                one with respect to x (sparda_indexer_kl's d_f, say).
  * With (a, b) pair j of a row at position p and w = p freq[j]:
  *   y_a = scale (x_a cos w - x_b sin w), y_b = scale (x_a sin w + x_b cos w);
- * backward: w negated.  The angle is reduced in float64, products in float32, one rounding.
+ * backward: w negated.  The angle is formed and reduced in float64 (|w| below 2^31 leaves 2^-20 of a radian),
+ * products in float32, one rounding.
  */
 int sparda_rotate(const sparda_rope* rope, int32_t type, int32_t batch, int32_t n_heads, int64_t n_tok,
                   const sparda_rows* x, const int32_t* pos, int64_t pos_ld, const sparda_rows* y, int32_t backward,
@@ -624,8 +625,8 @@ typedef struct sparda_pages {
  *   q, q_out   : bf16 rows [B][Hq][n_max][D]: the queries, and where they go turned; in place is allowed.
  *                Both or neither NULL.
  *   f, f_out   : bf16 rows [B][Hkv][n_max][D]: the same for the Forecast rows.
- *   t_new  out : int32 [B] device: t_ctx plus the tokens taken (t_ctx itself for an absent sequence); not
- *                the array t_ctx.
+ *   t_new  out : int32 [B] device: t_ctx plus the tokens taken (t_ctx itself for an absent sequence); neither
+ *                the array t_ctx nor n_new.
  * K is rounded to bf16 once, after the rotation; the means are those of the rounded keys, with the bits of
  * sparda_compress_keys; a window is written when it ends in (t_ctx, t_new] and all its tokens have pages.
  * Rows of q_out and f_out past a sequence's tokens, and whatever else the pages hold, are left as they were.

@@ -209,7 +209,8 @@ int sparda_paged_append(const sparda_shape* shape, const sparda_pages* pages, co
   if ((n_new && (rc = check_dev(n_new, "n_new", 4))) || (rc = check_dev(t_ctx, "t_ctx", 4)) ||
       (rc = check_dev(t_new, "t_new", 4)))
     return rc;
-  if (t_new == t_ctx) return fail(SPARDA_ERR_INVALID_ARG, "t_new is t_ctx: other workgroups still read it");
+  if (t_new == t_ctx || t_new == n_new)
+    return fail(SPARDA_ERR_INVALID_ARG, "t_new is t_ctx or n_new: other workgroups still read it");
   const int B = shape->batch, H = shape->n_kv_heads, Hq = H * shape->group_size;
   if ((q == nullptr) != (q_out == nullptr)) return fail(SPARDA_ERR_INVALID_ARG, "q and q_out: both or neither");
   if ((f == nullptr) != (f_out == nullptr)) return fail(SPARDA_ERR_INVALID_ARG, "f and f_out: both or neither");

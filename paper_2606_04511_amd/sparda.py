@@ -129,18 +129,30 @@ class SpardaPages:
         if not pools or len({x.shape[0] for x in pools}) != 1:
             raise ValueError("k, v and k_cmp have the same number of pages")
         for x, name in ((k, "k"), (v, "v"), (k_cmp, "k_cmp")):
-            if x is not None and (x.dtype != torch.bfloat16 or x.dim() != 4 or not x[0].is_contiguous()):
+            if x is not None and (x.dtype != torch.bfloat16 or x.dim() != 4 or x.shape[3] != 128 or not x[0].is_contiguous()):
                 raise ValueError(f"{name}: bf16 [n_pages][Hkv][tokens][128] with dense pages")
-        if (k is None) != (v is None) or (k is not None and k.stride(0) != v.stride(0)):
+        if (k is None) != (v is None) or (k is not None and (k.stride(0) != v.stride(0) or k.shape != v.shape)):
             raise ValueError("k and v come together, with one stride between pages")
+        if k is not None and k.shape[2] != page_size:
+            raise ValueError(f"pages of {k.shape[2]} tokens, page_size {page_size}")
         if k_cmp is not None and not k_cmp.is_contiguous():
             raise ValueError("k_cmp is not dense")
         if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1:
             raise ValueError("table: int32 [B][pages of a sequence]")
+        self.page_size, self.n_seqs = page_size, table.shape[0]
+        self.kv_heads = None if k is None else k.shape[1]
+        self.cmp = None if k_cmp is None else (k_cmp.shape[1], k_cmp.shape[2])
         self.tensors = (table, k, v, k_cmp)
         self.c = _CPages(ctypes.sizeof(_CPages), page_size, pools[0].shape[0],
                          table.stride(0) if table.shape[0] > 1 else table.shape[1], 0 if k is None else k.stride(0),
                          _p(table), _p(k), _p(v), _p(k_cmp))
+
+    def check(self, shape: SpardaShape):
+        """The pages are those of such a shape."""
+        if (self.n_seqs < shape.batch or self.kv_heads not in (None, shape.n_kv_heads) or
+                self.cmp not in (None, (shape.n_kv_heads, self.page_size // shape.cmp_stride))):
+            raise ValueError(f"pages of {self.n_seqs} sequences, {self.kv_heads} KV heads, {self.cmp} heads and keys of a page "
+                             f"do not go with {shape}")
 
 
 class SpardaError(RuntimeError):
@@ -463,6 +475,7 @@ def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int
                         f_out, t_new, stream=None):
     cs, b, h, bf = shape.c(), shape.batch, shape.n_kv_heads, torch.bfloat16
     kv, hq = (b, h, n_max, 128), (b, shape.n_q_heads, n_max, 128)
+    pages.check(shape)
     _here(rope.freq if rope else None, pages.tensors[0], n_new, t_ctx, k_new, v_new, q, q_out, f, f_out, t_new)
     _check(load().sparda_paged_append(ctypes.byref(cs), ctypes.byref(pages.c), ctypes.byref(rope.c) if rope else None, n_max,
                                       _p(n_new), _p(t_ctx), _rows(k_new, "k_new", kv, bf), _rows(v_new, "v_new", kv, bf),
@@ -475,6 +488,7 @@ def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max:
     cs = shape.c()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
+    pages.check(shape)
     _here(pages.tensors[0], f, t_ctx, sel, cnt, ws)
     _check(load().sparda_paged_select(ctypes.byref(cs), ctypes.byref(pages.c), _p(f), _p(t_ctx), t_max, _p(sel), _p(cnt),
                                       _p(ws), ws_bytes, _stream(stream)), "sparda_paged_select")
@@ -485,6 +499,7 @@ def sparda_paged_attn(shape: SpardaShape, pages: SpardaPages, q, t_ctx, t_max: i
     cs = shape.c()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
+    pages.check(shape)
     _here(pages.tensors[0], q, t_ctx, sel, cnt, o, ws)
     _check(load().sparda_paged_attn(ctypes.byref(cs), ctypes.byref(pages.c), _p(q), _p(t_ctx), t_max, _p(sel), _p(cnt),
                                     float(sm_scale), _p(o), _p(ws), ws_bytes, _stream(stream)), "sparda_paged_attn")

@@ -35,6 +35,9 @@ class Raw:
     def __init__(self, c):
         self.c, self.tensors, self.freq = c, (None,), None
 
+    def check(self, shape):
+        pass
+
 
 def pages(**kw):
     base = dict(size=ctypes.sizeof(sp._CPages), page_size=64, n_pages=256, table_ld=128, page_ld=8 * 64 * 128, table=FAKE,
@@ -105,7 +108,8 @@ def test_append_refusals():
     for kw, status in ROPES:
         assert rc_of(f, *replaced(good, a2=rope(**kw))) == status, kw
     for at, status in ((dict(a0=shape(head_dim=64)), UNSUP), (dict(a3=0), BAD), (dict(a3=8193), BAD), (dict(a4=FAKE + 1), BAD),
-                       (dict(a5=None), BAD), (dict(a12=None), BAD), (dict(a12=FAKE), BAD), (dict(a8=None), BAD),
+                       (dict(a5=None), BAD), (dict(a12=None), BAD), (dict(a12=FAKE), BAD),
+                       (dict(a4=FAKE * 2), BAD), (dict(a8=None), BAD),
                        (dict(a9=None), BAD), (dict(a10=None), BAD), (dict(a11=None), BAD),
                        (dict(a9=(FAKE, 1 << 22, 1 << 13, 128)), BAD), (dict(a11=(FAKE, 1 << 20, 1 << 13, 128)), BAD),
                        (dict(a0=shape(batch=8000, t_cap=1 << 20), a1=pages(table_ld=1 << 14), a3=1 << 20), UNSUP)):
@@ -161,9 +165,17 @@ def test_handles_check_their_tensors():
     c = sp.SpardaPages(64, table, both[:, 0], both[:, 1]).c
     assert (c.n_pages, c.table_ld, c.page_ld) == (4, 3, 2 * 2 * 64 * 128)
     for args in ((64, table), (64, table, k, None), (64, table, k, k[:3]), (64, table.long(), k, k), (64, table.t(), k, k),
-                 (64, table, k.float(), k), (64, table, k.transpose(1, 2), k), (64, table, k, both[:, 0])):
+                 (64, table, k.float(), k), (64, table, k.transpose(1, 2), k), (64, table, k, both[:, 0]), (32, table, k, k),
+                 (64, table, k[..., :64], k[..., :64]), (64, table, k, k[:, :1].contiguous())):
         with pytest.raises(ValueError):
             sp.SpardaPages(*args)
+    kc = torch.zeros(4, 2, 4, 128, dtype=torch.bfloat16)
+    good = sp.SpardaPages(64, table, k, k, kc)
+    good.check(shape(n_kv_heads=2, cmp_kernel=32, cmp_stride=16))
+    for kw in (dict(n_kv_heads=2), dict(n_kv_heads=1, cmp_kernel=32, cmp_stride=16),
+               dict(batch=3, n_kv_heads=2, cmp_kernel=32, cmp_stride=16)):
+        with pytest.raises(ValueError):
+            good.check(shape(**kw))
     for freq in (torch.zeros(64), torch.zeros(63, dtype=torch.float64), torch.zeros(128, dtype=torch.float64)[::2]):
         with pytest.raises(ValueError):
             sp.SpardaRope(128, sp.SPARDA_ROPE_HALF, freq)
