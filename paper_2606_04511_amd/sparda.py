@@ -117,6 +117,7 @@ class SpardaRope:
         _expect(freq, "freq", torch.float64, rot_dim // 2)
         self.freq = freq
         self.c = _CRope(ctypes.sizeof(_CRope), rot_dim, layout, scale, _p(freq))
+        self.ref = ctypes.byref(self.c)
 
 
 class SpardaPages:
@@ -146,6 +147,7 @@ class SpardaPages:
         self.c = _CPages(ctypes.sizeof(_CPages), page_size, pools[0].shape[0],
                          table.stride(0) if table.shape[0] > 1 else table.shape[1], 0 if k is None else k.stride(0),
                          _p(table), _p(k), _p(v), _p(k_cmp))
+        self.ref = ctypes.byref(self.c)
 
     def check(self, shape: SpardaShape):
         """The pages are those of such a shape."""
@@ -268,10 +270,10 @@ def _rows(x, name: str, shape, dtype):
         return None
     if isinstance(x, tuple):
         return _pack_rows(x[0] or 0, *x[1:])
-    ld = x.stride()
-    if x.shape != shape or x.dtype != dtype or ld[3] != 1:
+    b, h, t, d = x.stride()  # (ValueError where there are not four)
+    if d != 1 or x.shape != shape or x.dtype != dtype:
         raise ValueError(f"{name}: {tuple(shape)} of {dtype} expected, its last dimension dense")
-    return _pack_rows(x.data_ptr(), ld[0], ld[1], ld[2])
+    return _pack_rows(x.data_ptr(), b, h, t)
 
 
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -467,17 +469,17 @@ def sparda_rotate(rope: SpardaRope, type: int, batch: int, n_heads: int, n_tok: 
                   backward: bool = False, stream=None):
     dtype, size = torch.float32 if type == SPARDA_F32 else torch.bfloat16, (batch, n_heads, n_tok, 128)
     _here(rope.freq, x, y, pos)
-    _check(load().sparda_rotate(ctypes.byref(rope.c), type, batch, n_heads, n_tok, _rows(x, "x", size, dtype), _p(pos),
+    _check(load().sparda_rotate(rope.ref, type, batch, n_heads, n_tok, _rows(x, "x", size, dtype), _p(pos),
                                 pos_ld, _rows(y, "y", size, dtype), int(backward), _stream(stream)), "sparda_rotate")
 
 
 def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int, n_new, t_ctx, k_new, v_new, q, q_out, f,
                         f_out, t_new, stream=None):
     cs, b, h, bf = shape.c(), shape.batch, shape.n_kv_heads, torch.bfloat16
-    kv, hq = (b, h, n_max, 128), (b, shape.n_q_heads, n_max, 128)
+    kv, hq = (b, h, n_max, 128), (b, h * shape.group_size, n_max, 128)
     pages.check(shape)
     _here(rope.freq if rope else None, pages.tensors[0], n_new, t_ctx, k_new, v_new, q, q_out, f, f_out, t_new)
-    _check(load().sparda_paged_append(ctypes.byref(cs), ctypes.byref(pages.c), ctypes.byref(rope.c) if rope else None, n_max,
+    _check(load().sparda_paged_append(ctypes.byref(cs), pages.ref, rope.ref if rope else None, n_max,
                                       _p(n_new), _p(t_ctx), _rows(k_new, "k_new", kv, bf), _rows(v_new, "v_new", kv, bf),
                                       _rows(q, "q", hq, bf), _rows(q_out, "q_out", hq, bf), _rows(f, "f", kv, bf),
                                       _rows(f_out, "f_out", kv, bf), _p(t_new), _stream(stream)), "sparda_paged_append")
@@ -490,7 +492,7 @@ def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max:
         ws_bytes = ws.numel() * ws.element_size()
     pages.check(shape)
     _here(pages.tensors[0], f, t_ctx, sel, cnt, ws)
-    _check(load().sparda_paged_select(ctypes.byref(cs), ctypes.byref(pages.c), _p(f), _p(t_ctx), t_max, _p(sel), _p(cnt),
+    _check(load().sparda_paged_select(ctypes.byref(cs), pages.ref, _p(f), _p(t_ctx), t_max, _p(sel), _p(cnt),
                                       _p(ws), ws_bytes, _stream(stream)), "sparda_paged_select")
 
 
@@ -501,5 +503,5 @@ def sparda_paged_attn(shape: SpardaShape, pages: SpardaPages, q, t_ctx, t_max: i
         ws_bytes = ws.numel() * ws.element_size()
     pages.check(shape)
     _here(pages.tensors[0], q, t_ctx, sel, cnt, o, ws)
-    _check(load().sparda_paged_attn(ctypes.byref(cs), ctypes.byref(pages.c), _p(q), _p(t_ctx), t_max, _p(sel), _p(cnt),
+    _check(load().sparda_paged_attn(ctypes.byref(cs), pages.ref, _p(q), _p(t_ctx), t_max, _p(sel), _p(cnt),
                                     float(sm_scale), _p(o), _p(ws), ws_bytes, _stream(stream)), "sparda_paged_attn")

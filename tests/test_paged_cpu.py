@@ -33,7 +33,7 @@ class Raw:
     """A handle whose struct a test fills itself."""
 
     def __init__(self, c):
-        self.c, self.tensors, self.freq = c, (None,), None
+        self.c, self.ref, self.tensors, self.freq = c, ctypes.byref(c), (None,), None
 
     def check(self, shape):
         pass
