@@ -665,7 +665,7 @@ int sparda_paged_select(const sparda_shape* shape, const sparda_pages* pages, co
  *                not depend on the lengths beyond t_max.
  * o = softmax(sm_scale q K^T) V over the tokens t < t_ctx of the listed blocks, or all of them: bf16 inputs,
  * float32 accumulation and online softmax; a weight enters the product with V to within 2^-16 of itself.
- * Whatever the pages hold from t_ctx on has no effect.  A NaN in a query, or in a key or value that it attends, makes
+ * Whatever the pages hold from t_ctx on has no effect.  A token whose score is -inf weighs nothing.  A NaN in a query, or in a key or value that it attends, makes
  * what depends on it NaN; an infinite value that is attended makes its element of the output infinite or NaN.
  * Deterministic.
  */

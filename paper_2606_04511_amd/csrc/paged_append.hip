@@ -9,6 +9,10 @@
 //
 // A window's mean has the bits of compress_kernel (compress.hip): the float64 sums run in its order, rows r + 16 x
 // first, then over r.
+//
+// What bounds it: for a token per sequence the chain length -> page -> rows -> stores (5.4 us for one sequence, 5.7 for
+// 32); for prompts the memory's rate (13289 tokens of 56 heads, 381 MB: 73 us on one input, 5.2 TB/s, 80 on inputs in turn).
+// Of those the angles, which every KV head forms again, are 6 us, the windows 7.
 #include "rotary.hpp"
 
 namespace sparda {

@@ -12,7 +12,13 @@
 // heads as columns: K goes through 8 KiB of the wavefront's LDS (whole rows in, fragments of 16 bytes out, swizzled).
 // A lane then holds 8 tokens' scores of one head, which is the B operand of O^T += V^T P^T when the lane's sixteen
 // loads those 8 tokens of V, 16 bytes (8 elements) of each; the 8 x 8 corner is turned in registers and element j of every
-// lane's eight is the j-th A operand, 16 rows of it: lane (g, c) ends with elements 32 g .. 32 g + 31 of head c.
+// lane's eight is the j-th A operand, 16 rows of it: lane (g, c) ends with elements 32 g .. 32 g + 31 of head c.  The weights
+// enter the product as two bf16 numbers, which costs matrix time that is free here (they are busy for less than a tenth).
+// The next unit's K and V are under way in registers during a unit's products: 16 KiB per wavefront, 128 KiB per CU.
+//
+// What bounds it: the memory's rate of block reads.  8 sequences of 18K to 33K tokens, 8 KV heads (839 MB): 126 us, 6.7 TB/s,
+// and 4 for the join; 256 rows of 64 blocks (537 MB): 79 us, 6.8 TB/s.  Small calls are chains: length -> page -> K -> V ->
+// join in LDS -> second launch, 8.9 us for 8 rows of 4K; a row of a few tokens 4.7.
 #include <type_traits>
 
 #include "device_util.hpp"

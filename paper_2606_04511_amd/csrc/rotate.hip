@@ -1,6 +1,10 @@
 // rotate.hip -- rotary positions of rows, or the gradient through them (the transposed rotation: the angle negated).
 //
-// Eight lanes per row (rotary.hpp); a group of eight lanes forms the angles of a token once and walks over its heads.
+// Eight lanes per row (rotary.hpp); a group of eight lanes forms the angles of a token once and walks over its heads, with
+// the loads of several heads under way.  Rows are read and written once, past the caches.
+//
+// What bounds it: the memory's rate for a copy (32717 tokens of 32 heads: 536 MB in 101 us, 5.3 TB/s; a copy of as much takes
+// 104 us; with ordinary loads and stores it was 114 us), for few rows the launch (2048 float32 rows: 4 us).
 #include "rotary.hpp"
 
 namespace sparda {

@@ -270,6 +270,8 @@ SELECT = [
     ((270000,), 1, 64, 1, 2, 64, (32, 16)),                                   # 4216: radix passes over memory
     ((200000,), 1, 40, 1, 2, 65536, (64, 64)),                                # 3123
     (tuple(range(64, 64 + 40 * 37, 37)), 8, 9, 1, 2, 64, (64, 64)),           # 320 rows
+    ((1100000, 70), 1, 64, 1, 2, 64, (64, 64)),                               # 17185: more than LDS holds
+    ((5000, 4000) * 14, 7, 9, 1, 2, 32, (32, 16)),                            # 196 rows, (32, 16), one launch
 ]
 
 
@@ -379,6 +381,10 @@ DENSE = [
     (tuple(range(1, 300, 7)), 4, 3, 16),
     ((5, 9) * 300, 2, 1, 16),            # more sequences than threads of a workgroup
     ((0, -1) * 20, 2, 4, 16),            # nothing at all
+    ((5000,) + tuple(range(0, 127)), 2, 3, 32),                  # one long context among short ones
+    (tuple(range(0, 40)) * 13 + (5000, 700), 1, 4, 16),          # the same with more sequences than threads
+    (tuple(range(2300, 500, -55)), 8, 4, 64),                    # 264 rows, most of them long
+    ((3, 9000, 0, 4100, 31) * 13, 4, 16, 128),                   # long rows that share workgroups with short ones
 ]
 
 
@@ -418,6 +424,8 @@ SPARSE = [
     (tuple(range(1, 2000, 29)) + (0, -9), 4, 1, 64, 32, "sorted"),  # lists longer than most contexts
     (tuple(range(1, 2000, 29)) + (0, -9), 4, 1, 70, 32, "twice"),
     ((100000,), 1, 2, 1000, 64, "sorted"),
+    ((2700, 3, 0) + tuple(range(2600, 2700)), 3, 4, 40, 64, "sorted"),  # 309 rows of up to 40 blocks
+    ((2700, 3, 0) + tuple(range(2600, 2700)), 3, 2, 40, 16, "mixed"),
 ]
 
 
@@ -486,6 +494,17 @@ def test_attention_skips_what_has_no_page(dev):
     got = run_attn(dev, shape_of(4, 2, 3, k=8, t_cap=1000), pages, q, t, 1000, sel, cnt)
     check(got, *ref.attn(q[:, :, 0], k, v, table, t, page, sel, cnt, ref.SCALE))
     assert (got[2] == 0).all()
+
+
+def test_attention_of_interleaved_pools(dev):
+    """K and V as slices of one pool [n_pages][2][Hkv][P][128]."""
+    gen, rng, t_ctx, page = torch.Generator().manual_seed(19), random.Random(19), (300, 77), 32
+    table, n_pages = table_of(rng, 2, 300, page, lens=t_ctx)
+    k, v = pools(gen, table, t_ctx, n_pages, 2, page)
+    pool = torch.stack((k, v), 1).to(dev)
+    q, t = torch.randn(2, 8, 1, D, generator=gen).to(BF), torch.tensor(t_ctx, dtype=torch.int32)
+    got = run_attn(dev, shape_of(2, 2, 4, t_cap=300), sp.SpardaPages(page, table.to(dev), pool[:, 0], pool[:, 1]), q, t, 300, None, None)
+    check(got, *ref.attn(q[:, :, 0], k, v, table, t, page, None, None, ref.SCALE))
 
 
 def test_attention_nan_and_infinity(dev):
