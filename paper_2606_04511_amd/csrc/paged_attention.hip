@@ -139,11 +139,23 @@ struct Running {
   float m, l;
 };
 
+// The beginning of a row's list: its length and, in lane i, entry i.  The two loads do not wait for each other (entries
+// past the length, which k_total bounds, are not used).
+struct Listed {
+  int cnt, entry;
+};
+template <bool kSparse>
+__device__ __forceinline__ Listed list_of(const PagedAttnArgs& a, int64_t row) {
+  if constexpr (!kSparse) return {0, -1};
+  const int lane = threadIdx.x & 63;
+  return {a.cnt[row], a.sel[row * a.k_total + min(lane, a.k_total - 1)]};
+}
+
 // The wavefront's units [u0, u1) of row r (counted within the row; those of a list are the blocks that it names, in its
 // order, each once).  list: 64 block indices of the wavefront's own LDS.
 template <bool kSparse>
-__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, int u0, int u1, char* kbuf, int16_t* list,
-                                       Running* run) {
+__device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, const Listed& listed, int u0, int u1, char* kbuf,
+                                       int16_t* list, Running* run) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) run->acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -293,15 +305,19 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, i
     }
   } else {
     const int16_t* sel = a.sel + row * a.k_total;
-    int cnt = a.cnt[row];
-    cnt = cnt > a.k_total ? a.k_total : cnt;
+    const int cnt = min(listed.cnt, a.k_total);
     bool ascending = true;  // so far: a list that ascends strictly names no block twice
     int before = 0;         // blocks that the entries before i0 name
+    int entry = listed.entry, last_entry = -1;
     for (int i0 = 0; i0 < cnt && 2 * before < u1; i0 += 64) {
       const int i = i0 + lane;
-      const int blk = i < cnt ? sel[i] : -1;
+      if (i0 > 0) entry = sel[min(i, cnt - 1)];
+      const int blk = i < cnt ? entry : -1;
       bool in = blk >= 0 && (int64_t)blk * 64 < r.t;
-      if (__ballot(i > 0 && i < cnt && sel[max(min(i, cnt - 1) - 1, 0)] >= blk) != 0ull) ascending = false;
+      int prev = __shfl_up(entry, 1, 64);
+      if (lane == 0) prev = last_entry;
+      last_entry = __shfl(entry, 63, 64);
+      if (__ballot(i > 0 && i < cnt && prev >= blk) != 0ull) ascending = false;
       if (!ascending)
         for (int x = 0; x < i && in; ++x)
           if (sel[x] == blk) in = false;
@@ -430,10 +446,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
   RowAt r;
   uint32_t w0, w1, piece = 0;
   Starts st = {0u, 0u};
+  Listed listed = {0, -1};
   if (n_splits > 0) {
     const uint32_t row = blockIdx.x / (uint32_t)n_splits, split = blockIdx.x % (uint32_t)n_splits;
     r.b = (int)(row / (uint32_t)a.n_kv_heads);
     r.h = (int)(row % (uint32_t)a.n_kv_heads);
+    listed = list_of<kSparse>(a, row);  // (requested beside the length)
     r.t = attn_context(a, r.b);
     r.u0 = 0;
     r.units = units_of(a, r.t);
@@ -477,7 +495,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
       r = line_row(a, per, st, pre, p0);
       for (uint32_t u = p0;;) {
         const uint32_t end = r.end() < p1 ? r.end() : p1;
-        attend<kSparse>(a, r, (int)(u - r.u0), (int)(end - r.u0), kbuf[wave], lists[wave], &run);
+        attend<kSparse>(a, r, list_of<kSparse>(a, (int64_t)r.b * a.n_kv_heads + r.h), (int)(u - r.u0), (int)(end - r.u0), kbuf[wave], lists[wave], &run);
         if (u == r.u0 && end == r.end())
           write_row(a, r, run);
         else if (c < a.group_size)
@@ -487,18 +505,20 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
         r = next_row(a, r);
       }
     }
+    listed = list_of<kSparse>(a, (int64_t)r.b * a.n_kv_heads + r.h);
   }
   // every row divided by the wavefronts
   for (uint32_t u = w0;;) {
     const uint32_t end = r.end() < w1 ? r.end() : w1;
     uint32_t v0, v1;
     share_of(end - u, wave, kPagedWaves, &v0, &v1);
-    attend<kSparse>(a, r, (int)(u - r.u0 + v0), (int)(u - r.u0 + v1), kbuf[wave], lists[wave], &run);
+    attend<kSparse>(a, r, listed, (int)(u - r.u0 + v0), (int)(u - r.u0 + v1), kbuf[wave], lists[wave], &run);
     const bool whole = n_splits > 0 ? n_splits == 1 : u == r.u0 && end == r.end();
     join_waves(a, r, run, kbuf, stat, whole, (int64_t)blockIdx.x * kPagedWaves * 2 + (u == w0 ? 0 : 1));
     u = end;
     if (u >= w1) return;
     r = next_row(a, r);
+    listed = list_of<kSparse>(a, (int64_t)r.b * a.n_kv_heads + r.h);
     __syncthreads();  // the results have been read
   }
 }
