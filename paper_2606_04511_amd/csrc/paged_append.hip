@@ -10,9 +10,9 @@
 // A window's mean has the bits of compress_kernel (compress.hip): the float64 sums run in its order, rows r + 16 x
 // first, then over r.
 //
-// What bounds it: for a token per sequence the chain length -> page -> rows -> stores (5.4 us for one sequence, 5.7 for
-// 32); for prompts the memory's rate (13289 tokens of 56 heads, 381 MB: 73 us on one input, 5.2 TB/s, 80 on inputs in turn).
-// Of those the angles, which every KV head forms again, are 6 us, the windows 7.
+// What bounds it: for a token per sequence the chain length -> page -> rows -> stores (5.6 us for one sequence, 6.0 for
+// 32); for prompts the memory's rate (13289 tokens of 56 heads, 381 MB: 71 us, 5.4 TB/s).  Of those the angles, which every
+// KV head forms again, are 4 us, the windows 5.
 #include "rotary.hpp"
 
 namespace sparda {
@@ -37,7 +37,7 @@ template <int L>  // tokens of a window; its stride is 64 with L = 64, else 16
 __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, int slices) {
   constexpr int S = L == 64 ? 64 : 16, kBefore = L - S;
   const int tid = threadIdx.x, c = tid & 7, g = tid >> 3;
-  const Chunks ch = rotary_chunks(a.rope, c);
+  Slot<8> slot(a.rope, c);
   const int h = (int)(unit % a.n_kv_heads);
   const int64_t rest = unit / a.n_kv_heads;
   const int b = (int)(rest / slices);
@@ -55,34 +55,50 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
   if (first_end < L) first_end = L;
   const bool windows = a.pg.kc && first_end <= end;
   const int64_t low = windows ? first_end - L : from;  // the first key that a window needs
-  for (int rr = g; rr < 64 + kBefore; rr += 32) {
-    const int64_t tok = base - kBefore + rr;
-    if (tok < low || tok >= end) continue;
-    const int32_t page = page_of(a.pg, table, tok);
-    uint4 wa = make_uint4(0u, 0u, 0u, 0u), wb = wa;
-    if (tok >= t0) {
+  // the rows of a thread, their loads under way together
+  constexpr int kRows = (64 + kBefore + 31) / 32;
+  uint4 ka[kRows], kb[kRows], va[kRows], vb[kRows];
+  int32_t page[kRows];
+  bool used[kRows];
+#pragma unroll
+  for (int x = 0; x < kRows; ++x) {
+    const int64_t tok = base - kBefore + g + 32 * x;
+    used[x] = g + 32 * x < 64 + kBefore && tok >= low && tok < end;
+    page[x] = used[x] ? page_of(a.pg, table, tok) : -1;
+    ka[x] = kb[x] = va[x] = vb[x] = make_uint4(0u, 0u, 0u, 0u);
+    if (used[x] && tok >= t0) {
       const uint16_t* src = row_of(a.k_new, b, h, tok - t0);
-      wa = ld16_nt(src + 8 * ch.a);
-      wb = ld16_nt(src + 8 * ch.b);
-      Turns turn;
-      rotary_turns(a.rope, c, ch, tok, 1.f, &turn);
-      rotary_row(a.rope, ch, turn, wa, wb);
-      if (tok >= base && page >= 0) {
+      ka[x] = ld16_nt(src + 8 * slot.a);
+      kb[x] = ld16_nt(src + 8 * slot.b);
+      if (tok >= base) {
         const uint16_t* vs = row_of(a.v_new, b, h, tok - t0);
-        const uint4 va = ld16_nt(vs + 8 * c), vb = ld16_nt(vs + 8 * c + 64);
-        const int64_t at = token_at(a.pg, page, h, tok);
-        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * ch.a) = wa;
-        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * ch.b) = wb;
-        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c) = va;
-        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c + 64) = vb;
+        va[x] = ld16_nt(vs + 8 * c);
+        vb[x] = ld16_nt(vs + 8 * c + 64);
       }
-    } else if (page >= 0) {
-      const uint16_t* src = a.pg.k + token_at(a.pg, page, h, tok);
-      wa = ld16(src + 8 * ch.a);
-      wb = ld16(src + 8 * ch.b);
     }
-    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * ch.a) = wa;
-    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * ch.b) = wb;
+  }
+#pragma unroll
+  for (int x = 0; x < kRows; ++x) {
+    const int rr = g + 32 * x;
+    const int64_t tok = base - kBefore + rr;
+    if (!used[x]) continue;
+    if (tok >= t0) {
+      slot.angles(a.rope, tok, 1.f);
+      turn_pieces(a.rope, slot, ka[x], kb[x]);
+      if (tok >= base && page[x] >= 0) {
+        const int64_t at = token_at(a.pg, page[x], h, tok);
+        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * slot.a) = ka[x];
+        *reinterpret_cast<uint4*>(a.pg.k + at + 8 * slot.b) = kb[x];
+        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c) = va[x];
+        *reinterpret_cast<uint4*>(a.pg.v + at + 8 * c + 64) = vb[x];
+      }
+    } else if (page[x] >= 0) {
+      const uint16_t* src = a.pg.k + token_at(a.pg, page[x], h, tok);
+      ka[x] = ld16(src + 8 * slot.a);
+      kb[x] = ld16(src + 8 * slot.b);
+    }
+    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * slot.a) = ka[x];
+    *reinterpret_cast<uint4*>(lds + rr * 256 + 16 * slot.b) = kb[x];
   }
   if (!windows) return;
   __syncthreads();
@@ -90,8 +106,8 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
   const int n_win = (int)((end - first_end) / S) + 1, w = tid >> 6, d = 2 * (tid & 63);
   if (w >= n_win) return;
   const int64_t w_begin = first_end + w * S - L;
-  const int32_t page = page_of(a.pg, table, w_begin);
-  if (page < 0 || (L == 32 && page_of(a.pg, table, w_begin + 16) < 0)) return;
+  const int32_t at = page_of(a.pg, table, w_begin);
+  if (at < 0 || (L == 32 && page_of(a.pg, table, w_begin + 16) < 0)) return;
   const char* rows = lds + (w_begin - (base - kBefore)) * 256 + 2 * d;
   double s0 = 0.0, s1 = 0.0;
 #pragma unroll
@@ -106,7 +122,7 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
     s0 += p0;
     s1 += p1;
   }
-  *reinterpret_cast<uint32_t*>(a.pg.kc + key_at(a.pg, page, a.n_kv_heads, h, w_begin, L == 64 ? 6 : 4) + d) =
+  *reinterpret_cast<uint32_t*>(a.pg.kc + key_at(a.pg, at, a.n_kv_heads, h, w_begin, L == 64 ? 6 : 4) + d) =
       f64_to_bf16(s0 * (1.0 / L)) | (uint32_t)f64_to_bf16(s1 * (1.0 / L)) << 16;
 }
 
@@ -114,7 +130,7 @@ __device__ void append_block(const PagedAppendArgs& a, char* lds, int64_t unit, 
 __device__ void append_turn(const PagedAppendArgs& a, int64_t grp, int64_t n_groups, int heads) {
   if (grp >= n_groups) return;
   const int c = threadIdx.x & 7;
-  const Chunks ch = rotary_chunks(a.rope, c);
+  Slot<8> slot(a.rope, c);
   const int hq = a.q.data ? a.n_kv_heads * a.group_size : 0, hf = a.f.data ? a.n_kv_heads : 0;
   const int64_t tokens = (int64_t)a.batch * a.n_max;
   const int64_t tok = grp % tokens;
@@ -122,16 +138,25 @@ __device__ void append_turn(const PagedAppendArgs& a, int64_t grp, int64_t n_gro
   const int b = (int)(tok / a.n_max), j = (int)(tok % a.n_max);
   const int64_t t0 = a.t_ctx[b];
   if (j >= new_tokens(a, b, t0)) return;
-  Turns turn;
-  rotary_turns(a.rope, c, ch, t0 + j, 1.f, &turn);
-  for (int h = h0; h < h1; ++h) {
-    const bool isq = h < hq;
-    const uint16_t* x = isq ? row_of(a.q, b, h, j) : row_of(a.f, b, h - hq, j);
-    uint16_t* y = const_cast<uint16_t*>(isq ? row_of(a.q_out, b, h, j) : row_of(a.f_out, b, h - hq, j));
-    uint4 wa = ld16_nt(x + 8 * ch.a), wb = ld16_nt(x + 8 * ch.b);
-    rotary_row(a.rope, ch, turn, wa, wb);
-    *reinterpret_cast<uint4*>(y + 8 * ch.a) = wa;
-    *reinterpret_cast<uint4*>(y + 8 * ch.b) = wb;
+  slot.angles(a.rope, t0 + j, 1.f);
+  // the loads of four heads under way
+  for (int h = h0; h < h1; h += 4) {
+    uint4 wa[4], wb[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (h + e >= h1) break;
+      const uint16_t* x = h + e < hq ? row_of(a.q, b, h + e, j) : row_of(a.f, b, h + e - hq, j);
+      wa[e] = ld16_nt(x + 8 * slot.a);
+      wb[e] = ld16_nt(x + 8 * slot.b);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (h + e >= h1) break;
+      uint16_t* y = const_cast<uint16_t*>(h + e < hq ? row_of(a.q_out, b, h + e, j) : row_of(a.f_out, b, h + e - hq, j));
+      turn_pieces(a.rope, slot, wa[e], wb[e]);
+      *reinterpret_cast<uint4*>(y + 8 * slot.a) = wa[e];
+      *reinterpret_cast<uint4*>(y + 8 * slot.b) = wb[e];
+    }
   }
 }
 
@@ -152,8 +177,7 @@ hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream) {
   const int64_t kv_units = (int64_t)a.batch * a.n_kv_heads * slices;
   const int n_heads = (a.q.data ? a.n_kv_heads * a.group_size : 0) + (a.f.data ? a.n_kv_heads : 0);
   const int64_t tokens = (int64_t)a.batch * a.n_max;
-  int64_t heads = tokens * n_heads / 65536;
-  heads = heads < 1 ? 1 : heads > n_heads ? n_heads : heads;
+  const int64_t heads = n_heads ? rotary_heads(tokens * n_heads, n_heads) : 1;
   const int64_t groups = n_heads ? tokens * ((n_heads + heads - 1) / heads) : 0;
   const dim3 grid((unsigned)(kv_units + (groups + 31) / 32)), block(256);
   if (a.grid.l == 64)
