@@ -90,8 +90,9 @@ inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32
 }
 
 // How an attention call is cut.  The work of a row (a sequence's KV head) is counted in units of 32 tokens.  Either every
-// row has n_splits workgroups, which divide it evenly; or (n_splits 0) the rows lie one behind the other on a line, which is
-// cut into equal pieces whatever the lengths are, at the price of a scan over the lengths and a second launch (about 7 us).
+// row has n_splits workgroups, which divide it evenly; or (n_splits -1) every row has a wavefront; or (0) the rows lie one
+// behind the other on a line, which is cut into equal pieces whatever the lengths are, at the price of a scan over the lengths
+// and a second launch (about 7 us).
 //
 // The host knows the longest context only.  A workgroup alone reads about 50 GB/s, 0.33 us per unit: up to 64 units of the
 // longest row per workgroup, workgroups per row cost at most 20 us where all other rows are short, and are faster where
@@ -99,8 +100,12 @@ inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32
 // rows of 1000 24 and 19; 512 rows of 1000 with 4 heads 42 and 35, with 16 heads 55 and 37; 1600 rows of 1000 113 and 101;
 // but 320 rows of 2000 46 and 49, the second round being short.  Rows of the same length need no line: those of one
 // sequence, or of lists that are shorter than the contexts, while they fill at most one round of workgroups (256 rows of 64
-// blocks 85 and 82; 320 rows 107 and 122).  Many rows of a few units go to single wavefronts on the line (3200 rows of 100
-// tokens 41 and 54 us; with 16 heads, whose partial results weigh more, 66 and 59).
+// blocks 85 and 82; 320 rows 107 and 122).
+//
+// Many short rows have a wavefront each, the more units the more rows there are, up to 16 units (a wavefront alone needs 35
+// us for them).  Workgroups per row and a wavefront (us, contexts up to t): 320 rows of t = 60 7.9 and 7.1, of 100 8.3 and
+// 10.4; 800 rows of 100 15.8 and 12.7, of 300 24.7 and 27.4; 1600 rows of 100 26 and 14.6, of 300 43 and 34, of 500 61 and
+// 54; 3200 rows of 100 40 and 27, of 500 113 and 107.
 constexpr int kPagedWaves = 8;    // wavefronts of a workgroup
 constexpr int kPagedMaxWgs = 256; // one workgroup per CU
 // Units of a row of t tokens, of which a list of k_total blocks (0: no list) may name a part.
@@ -111,17 +116,19 @@ __host__ __device__ inline uint32_t paged_units(int64_t t, int32_t k_total) {
   return 2 * (uint32_t)(blocks < k_total ? blocks : k_total);
 }
 struct PagedPlan {
-  int32_t n_wgs, n_splits;
+  int32_t n_wgs, n_splits;  // n_splits 0: the line, -1: a wavefront per row
   bool joined;  // there may be partial results
 };
-inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int32_t group_size, int64_t t_max, int32_t k_total) {
+inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int64_t t_max, int32_t k_total) {
   const int64_t rows = (int64_t)batch * n_kv_heads, units = paged_units(t_max, k_total);
   int64_t s = rows <= kPagedMaxWgs && units > 16 ? kPagedMaxWgs / rows : 1;
   const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
   s = s < most ? s : most;
   const bool alike = rows <= kPagedMaxWgs && (batch == 1 || k_total > 0);
-  const bool tiny = rows > 1024 && units <= 8 && group_size <= 8;
-  if (alike || (units <= 64 * s && !tiny)) return {(int32_t)(rows * s), (int32_t)s, s > 1};
+  const int64_t rounds = (rows + kPagedMaxWgs - 1) / kPagedMaxWgs;
+  if (units <= (rounds >= 6 ? 16 : rounds >= 4 ? 6 : rounds >= 2 ? 2 : 0))
+    return {(int32_t)((rows + kPagedWaves - 1) / kPagedWaves), -1, false};
+  if (alike || units <= 64 * s) return {(int32_t)(rows * s), (int32_t)s, s > 1};
   const int64_t wgs = (rows * units + kPagedWaves - 1) / kPagedWaves;
   return {(int32_t)(wgs < kPagedMaxWgs ? wgs : kPagedMaxWgs), 0, true};
 }

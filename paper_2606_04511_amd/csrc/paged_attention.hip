@@ -2,11 +2,12 @@
 // context, for sequences of different lengths whose K and V lie in pages (paper Sec. 4.1, Eq. 5).
 //
 // A row is a sequence's KV head with its G query heads; its work is counted in units of 32 tokens.  Where the rows are few
-// and about as long (paged_attn_plan), a row has its own workgroups, which divide it evenly.  Otherwise the rows lie one
-// behind the other on a line, which is cut into equal pieces, one per wavefront, whatever the lengths are; where a workgroup's
-// piece holds long rows, its wavefronts divide each of them instead.  A wavefront goes over its units
-// once with a running maximum and sum per head; those of a workgroup that share a row join their results in LDS.  A row
-// that ends up whole is written; the results of the others go to the workspace and paged_join_kernel joins them.
+// and about as long (paged_attn_plan), a row has its own workgroups, which divide it evenly; where they are many and short,
+// a wavefront.  Otherwise the rows lie one behind the other on a line, which is cut into equal pieces, one per wavefront,
+// whatever the lengths are; where a workgroup's piece holds long rows, its wavefronts divide each of them instead.  A
+// wavefront goes over its units once with a running maximum and sum per head; those of a workgroup that share a row join
+// their results in LDS.  A row that ends up whole is written; the results of the others go to the workspace and
+// paged_join_kernel joins them.
 //
 // A unit is two slices of 16 tokens, the smallest page.  S^T = K Q^T on the matrix cores with 16 tokens as rows and the
 // heads as columns: K goes through 8 KiB of the wavefront's LDS (whole rows in, fragments of 16 bytes out, swizzled).
@@ -433,7 +434,7 @@ __device__ __forceinline__ void share_of(uint32_t n, int w, int parts, uint32_t*
   *v1 = *v0 + each < n ? *v0 + each : n;
 }
 
-// n_splits > 0: n_splits workgroups per row; 0: the line.
+// n_splits > 0: n_splits workgroups per row; -1: a wavefront per row; 0: the line.
 template <bool kSparse>
 __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a, int n_splits, int per) {
   __shared__ __align__(16) char kbuf[kPagedWaves][32 * 256];
@@ -447,6 +448,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
   uint32_t w0, w1, piece = 0;
   Starts st = {0u, 0u};
   Listed listed = {0, -1};
+  if (n_splits < 0) {
+    const int64_t row = (int64_t)blockIdx.x * kPagedWaves + wave;
+    if (row >= (int64_t)a.batch * a.n_kv_heads) return;
+    listed = list_of<kSparse>(a, row);
+    r.b = (int)(row / a.n_kv_heads);
+    r.h = (int)(row % a.n_kv_heads);
+    r.t = attn_context(a, r.b);
+    attend<kSparse>(a, r, listed, 0, (int)units_of(a, r.t), kbuf[wave], lists[wave], &run);
+    write_row(a, r, run);
+    return;
+  }
   if (n_splits > 0) {
     const uint32_t row = blockIdx.x / (uint32_t)n_splits, split = blockIdx.x % (uint32_t)n_splits;
     r.b = (int)(row / (uint32_t)a.n_kv_heads);
@@ -633,7 +645,7 @@ __global__ __launch_bounds__(kWaves == 16 ? 1024 : 256) void paged_join_kernel(P
 hipError_t launch_paged_attn(const PagedAttnArgs& args, hipStream_t stream) {
   PagedAttnArgs a = args;
   if (!a.sel) a.k_total = 0;
-  const PagedPlan p = paged_attn_plan(a.batch, a.n_kv_heads, a.group_size, a.t_max, a.k_total);
+  const PagedPlan p = paged_attn_plan(a.batch, a.n_kv_heads, a.t_max, a.k_total);
   const int per = a.batch <= 64 ? 0 : (a.batch + kThreads - 1) / kThreads;
   const dim3 grid((unsigned)p.n_wgs), block(kThreads);
   if (a.sel)

@@ -385,6 +385,14 @@ DENSE = [
     (tuple(range(0, 40)) * 13 + (5000, 700), 1, 4, 16),          # the same with more sequences than threads
     (tuple(range(2300, 500, -55)), 8, 4, 64),                    # 264 rows, most of them long
     ((3, 9000, 0, 4100, 31) * 13, 4, 16, 128),                   # long rows that share workgroups with short ones
+    # many short rows, a wavefront each: the last workgroup partly filled, absent sequences, contexts up to the longest that
+    # go this way and one past it, for every number of rows
+    ((61, 0, 64, 33, -1, 1, 32) * 37, 1, 4, 64),
+    ((64, 0, 65, 33, -1, 1, 32) * 37, 1, 4, 64),
+    ((192, 17, 0, 100, 31) * 51 + (191,), 3, 5, 16),
+    ((193, 17, 0, 100, 31) * 51 + (191,), 3, 5, 16),
+    ((512, 3, 0, 510, 250, 64) * 32 + (481,), 8, 16, 128),
+    ((513, 3, 0, 510, 250, 64) * 32 + (481,), 8, 2, 128),
 ]
 
 
@@ -426,6 +434,9 @@ SPARSE = [
     ((100000,), 1, 2, 1000, 64, "sorted"),
     ((2700, 3, 0) + tuple(range(2600, 2700)), 3, 4, 40, 64, "sorted"),  # 309 rows of up to 40 blocks
     ((2700, 3, 0) + tuple(range(2600, 2700)), 3, 2, 40, 16, "mixed"),
+    ((64, 1, 0, 50, -4) * 53, 1, 4, 7, 64, "mixed"),                    # many rows of few blocks, a wavefront each
+    ((900, 3, 0, 510, 250, 64) * 22 + (700,), 6, 4, 3, 32, "sorted"),
+    ((900, 3, 0, 510, 250, 64) * 32 + (481,), 8, 16, 8, 16, "twice"),
 ]
 
 
