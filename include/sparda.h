@@ -630,7 +630,10 @@ typedef struct sparda_pages {
  * K is rounded to bf16 once, after the rotation; the means are those of the rounded keys, with the bits of
  * sparda_compress_keys; a window is written when it ends in (t_ctx, t_new] and all its tokens have pages.
  * Rows of q_out and f_out past a sequence's tokens, and whatever else the pages hold, are left as they were.
- * No page that receives a token may belong to two sequences; the buffers must not overlap.
+ * No page that receives a token or a compressed key may belong to two sequences; the buffers must not overlap.
+ * (The key of a window that begins in one page and ends in the next lies in the first, so of a prefix that
+ * sequences share the last page is each one's own copy, tokens and keys, where l_C > s_C; the pages
+ * before it are complete.)
  */
 int sparda_paged_append(const sparda_shape* shape, const sparda_pages* pages, const sparda_rope* rope, int32_t n_max,
                         const int32_t* n_new, const int32_t* t_ctx, const sparda_rows* k_new, const sparda_rows* v_new,
@@ -665,9 +668,9 @@ int sparda_paged_select(const sparda_shape* shape, const sparda_pages* pages, co
  *                not depend on the lengths beyond t_max.
  * o = softmax(sm_scale q K^T) V over the tokens t < t_ctx of the listed blocks, or all of them: bf16 inputs,
  * float32 accumulation and online softmax; a weight enters the product with V to within 2^-16 of itself.
- * Whatever the pages hold from t_ctx on has no effect.  A token whose score is -inf weighs nothing.  A NaN in a query, or in a key or value that it attends, makes
- * what depends on it NaN; an infinite value that is attended makes its element of the output infinite or NaN.
- * Deterministic.
+ * Whatever the pages hold from t_ctx on has no effect.  A token whose score is -inf weighs nothing.  A NaN in
+ * a query, or in a key or value that it attends, makes what depends on it NaN; an infinite value that is
+ * attended makes its element of the output infinite or NaN.  Deterministic.
  */
 int sparda_paged_attn(const sparda_shape* shape, const sparda_pages* pages, const void* q, const int32_t* t_ctx,
                       int64_t t_max, const int16_t* sel, const int16_t* cnt, float sm_scale, void* o, void* ws,

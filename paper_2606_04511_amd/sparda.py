@@ -140,7 +140,9 @@ class SpardaPages:
             raise ValueError("k_cmp is not dense")
         if table.dtype != torch.int32 or table.dim() != 2 or table.stride(1) != 1:
             raise ValueError("table: int32 [B][pages of a sequence]")
-        self.page_size, self.n_seqs = page_size, table.shape[0]
+        if len({x.device for x in (table, *pools)}) != 1:
+            raise ValueError("the table and the pools are on one device")
+        self.page_size, self.n_seqs, self.tokens = page_size, table.shape[0], table.shape[1] * page_size
         self.kv_heads = None if k is None else k.shape[1]
         self.cmp = None if k_cmp is None else (k_cmp.shape[1], k_cmp.shape[2])
         self.tensors = (table, k, v, k_cmp)
@@ -151,10 +153,10 @@ class SpardaPages:
 
     def check(self, shape: SpardaShape):
         """The pages are those of such a shape."""
-        if (self.n_seqs < shape.batch or self.kv_heads not in (None, shape.n_kv_heads) or
+        if (self.n_seqs < shape.batch or self.tokens < shape.t_cap or self.kv_heads not in (None, shape.n_kv_heads) or
                 self.cmp not in (None, (shape.n_kv_heads, self.page_size // shape.cmp_stride))):
-            raise ValueError(f"pages of {self.n_seqs} sequences, {self.kv_heads} KV heads, {self.cmp} heads and keys of a page "
-                             f"do not go with {shape}")
+            raise ValueError(f"pages of {self.n_seqs} sequences of {self.tokens} tokens, {self.kv_heads} KV heads, {self.cmp} "
+                             f"heads and keys of a page do not go with {shape}")
 
 
 class SpardaError(RuntimeError):
@@ -458,7 +460,7 @@ def sparda_rope_freqs(rot_dim: int, base: float, scaling: int = SPARDA_ROPE_PLAI
     freq = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
     scale = ctypes.c_float(0.0)
     if factors is not None:
-        factors = torch.as_tensor(factors, dtype=torch.float64).contiguous()
+        factors = torch.as_tensor(factors, dtype=torch.float64, device="cpu").contiguous()
         _expect(factors, "factors", torch.float64, rot_dim // 2)
     _check(load().sparda_rope_freqs(rot_dim, base, scaling, factor, t_train, low, high, _p(factors), _p(freq),
                                     ctypes.byref(scale)), "sparda_rope_freqs")

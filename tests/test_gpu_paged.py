@@ -272,6 +272,7 @@ SELECT = [
     (tuple(range(64, 64 + 40 * 37, 37)), 8, 9, 1, 2, 64, (64, 64)),           # 320 rows
     ((1100000, 70), 1, 64, 1, 2, 64, (64, 64)),                               # 17185: more than LDS holds
     ((5000, 4000) * 14, 7, 9, 1, 2, 32, (32, 16)),                            # 196 rows, (32, 16), one launch
+    (((16384 + 2) * 64,), 1, 64, 1, 2, 64, (64, 64)),                         # 16383: as many as LDS holds
 ]
 
 
@@ -334,6 +335,25 @@ def test_select_ties_missing_pages_and_odd_scores(dev):
     assert not set(sel[1].tolist()) & set(range(1, 30, 2))
     assert 5 in sel[2].tolist() and 10 not in sel[2].tolist()
     assert sel[3].tolist() == sorted(set(sel[3].tolist())) and sel[3].min() >= 0 and sel[3].max() < 40
+
+
+def test_select_of_many_rows_of_one_prefix(dev):
+    """200 sequences that share their pages, 8192 candidates of each in one launch."""
+    gen, B, k = torch.Generator().manual_seed(6), 200, 20
+    n_blk = 8192 + 3
+    shape, t_max = shape_of(B, 1, 1, k, 64 * n_blk), 64 * n_blk
+    table = torch.randperm(n_blk, generator=gen).int().expand(B, n_blk).contiguous()
+    f, kc = exact_rows(gen, B, 1, 1, D), exact_rows(gen, n_blk, 1, 1, D)
+    t = [t_max - 64 * (b % 7) - b for b in range(B)]
+    sel = torch.empty(B, 1, 1, k, dtype=torch.int16, device=dev)
+    cnt = torch.empty(B, 1, 1, dtype=torch.int16, device=dev)
+    sp.sparda_paged_select(shape, sp.SpardaPages(64, table.to(dev), k_cmp=kc.to(dev)), f.to(dev),
+                           torch.tensor(t, dtype=torch.int32, device=dev), t_max, sel, cnt,
+                           workspace(dev, shape, sp.SPARDA_OP_PAGED_SELECT, t_max))
+    keys = kc[table[0].long(), 0, 0]
+    assert cnt.flatten().tolist() == [k] * B
+    for b in range(0, B, 9):
+        assert sel[b, 0, 0].tolist() == ref.selection(f[b, 0, 0], keys[:t[b] // 64], t[b], k, 1, 2, (64, 64)), b
 
 
 # ---- attention -----------------------------------------------------------------------------------
@@ -661,6 +681,30 @@ def test_serving_loop_against_dense_caches(dev, page, grid):
                     o, w = ref.attn(qo[b:b + 1, :, 0].cpu(), kt, vt, ident, tt, cap, s_, c_, ref.SCALE)
                     check(out[b:b + 1, :, 0].cpu(), o, w)
         loop.t.copy_(loop.t_new)
+
+
+@pytest.mark.parametrize("page,grid", [(64, (64, 64)), (32, (32, 16))])
+def test_shared_prefix(dev, page, grid):
+    """Sequences that share the pages of a prefix, its last page copied: the same bits as with pages of their own."""
+    B, H, prefix = 3, 2, 5 * page
+    own, shared = (Loop(dev, B, H, 4, 6, 1024, page, grid, 9) for _ in range(2))
+    new = [x[:1].expand_as(x).contiguous() for x in own.draw(prefix)]
+    own.append(prefix, None, *new, torch.empty_like(new[2]), torch.empty_like(new[3]))
+    first = torch.tensor([prefix, 0, 0], dtype=torch.int32, device=dev)
+    shared.append(prefix, first, *new, torch.empty_like(new[2]), torch.empty_like(new[3]))
+    for b in range(1, B):
+        for pool in (shared.k, shared.v, shared.kc):
+            pool[shared.table[b, 4].long()] = pool[shared.table[0, 4].long()]
+        shared.table[b, :4] = shared.table[0, :4]
+    for n in (1, 40, 1, 1):
+        (kn, vn, q, f), t = own.draw(n), own.t_new.clone()
+        for loop in (own, shared):
+            loop.t.copy_(t)
+            loop.qo, loop.fo = torch.empty_like(q), torch.empty_like(f)
+            loop.append(n, None, kn, vn, q, f, loop.qo, loop.fo)
+            loop.attend(loop.qo[:, :, -1:].contiguous(), loop.fo[:, :, -1:].contiguous())
+        assert torch.equal(own.t_new, shared.t_new) and torch.equal(own.sel, shared.sel)
+        assert torch.equal(bits(own.o), bits(shared.o)) and torch.equal(bits(own.all), bits(shared.all))
 
 
 def test_captured_step_replays(dev):

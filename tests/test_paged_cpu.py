@@ -166,14 +166,16 @@ def test_handles_check_their_tensors():
     assert (c.n_pages, c.table_ld, c.page_ld) == (4, 3, 2 * 2 * 64 * 128)
     for args in ((64, table), (64, table, k, None), (64, table, k, k[:3]), (64, table.long(), k, k), (64, table.t(), k, k),
                  (64, table, k.float(), k), (64, table, k.transpose(1, 2), k), (64, table, k, both[:, 0]), (32, table, k, k),
-                 (64, table, k[..., :64], k[..., :64]), (64, table, k, k[:, :1].contiguous())):
+                 (64, table, k[..., :64], k[..., :64]), (64, table, k, k[:, :1].contiguous()),
+                 (64, table.to("meta"), k, k), (64, table, k, k.to("meta"))):
         with pytest.raises(ValueError):
             sp.SpardaPages(*args)
     kc = torch.zeros(4, 2, 4, 128, dtype=torch.bfloat16)
     good = sp.SpardaPages(64, table, k, k, kc)
-    good.check(shape(n_kv_heads=2, cmp_kernel=32, cmp_stride=16))
-    for kw in (dict(n_kv_heads=2), dict(n_kv_heads=1, cmp_kernel=32, cmp_stride=16),
-               dict(batch=3, n_kv_heads=2, cmp_kernel=32, cmp_stride=16)):
+    good.check(shape(n_kv_heads=2, cmp_kernel=32, cmp_stride=16, t_cap=192))
+    for kw in (dict(n_kv_heads=2, t_cap=192), dict(n_kv_heads=1, cmp_kernel=32, cmp_stride=16, t_cap=192),
+               dict(batch=3, n_kv_heads=2, cmp_kernel=32, cmp_stride=16, t_cap=192),
+               dict(n_kv_heads=2, cmp_kernel=32, cmp_stride=16, t_cap=256)):
         with pytest.raises(ValueError):
             good.check(shape(**kw))
     for freq in (torch.zeros(64), torch.zeros(63, dtype=torch.float64), torch.zeros(128, dtype=torch.float64)[::2]):
