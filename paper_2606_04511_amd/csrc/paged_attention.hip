@@ -319,9 +319,23 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, c
       if (lane == 0) prev = last_entry;
       last_entry = __shfl(entry, 63, 64);
       if (__ballot(i > 0 && i < cnt && prev >= blk) != 0ull) ascending = false;
-      if (!ascending)
-        for (int x = 0; x < i && in; ++x)
-          if (sel[x] == blk) in = false;
+      if (!ascending) {  // not a block that an earlier entry names
+        for (int x0 = 0; x0 <= i0; x0 += 64) {
+          list[lane] = (int16_t)(x0 < i0 ? sel[x0 + lane] : blk);
+          wave_lds_sync();
+          const int n = min(i - x0, 64);
+#pragma unroll 1
+          for (int x = 0; x < 64; x += 8) {
+            const uint4 w = *reinterpret_cast<const uint4*>(list + x);
+            const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+            uint32_t same = 0;  // bit e: entry x0 + x + e is the block
+#pragma unroll
+            for (int e = 0; e < 8; ++e) same |= (int)(int16_t)(y[e >> 1] >> 16 * (e & 1)) == blk ? 1u << e : 0u;
+            if (x < n && (same & ((n - x < 8 ? 1u << (n - x) : 256u) - 1u)) != 0u) in = false;
+          }
+          wave_lds_sync();
+        }
+      }
       const uint64_t named = __ballot(in);
       const int n = (int)__popcll(named);
       if (2 * (before + n) > u0) {
@@ -440,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(PagedAttnArgs a
   __shared__ __align__(16) char kbuf[kPagedWaves][32 * 256];
   __shared__ uint32_t pre[kThreads], sums[kPagedWaves];
   __shared__ float stat[kPagedWaves][16][2];
-  __shared__ int16_t lists[kPagedWaves][kSparse ? 64 : 1];
+  __shared__ __align__(16) int16_t lists[kPagedWaves][kSparse ? 64 : 1];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Running run;
