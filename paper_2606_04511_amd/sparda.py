@@ -87,16 +87,15 @@ class SpardaShape:
         object.__setattr__(self, "_c", None)  # the C struct below is of other values
 
     def c(self) -> _CShape:
-        c = self._c
-        if c is None:
-            c = self._make()
-            object.__setattr__(self, "_c", c)
-        return c
-
-    def _make(self) -> _CShape:
         return _CShape(ctypes.sizeof(_CShape), self.batch, self.n_kv_heads, self.group_size, self.head_dim,
                        self.block_size, self.cmp_kernel, self.cmp_stride, self.n_init, self.n_local, self.k_total,
                        self.t_cap, self.nc_cap)
+
+    def _struct(self) -> _CShape:
+        """c() of these values, made once (0.9 us); the calls below only read it."""
+        if self._c is None:
+            object.__setattr__(self, "_c", self.c())
+        return self._c
 
 
 class _CRope(ctypes.Structure):
@@ -295,20 +294,20 @@ def _stream(stream):
 
 def sparda_workspace_size(shape: SpardaShape, op: int, n_q: int, q_pos0: int) -> int:
     n = ctypes.c_size_t(0)
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_workspace_size(ctypes.byref(cs), op, n_q, q_pos0, ctypes.byref(n)), "sparda_workspace_size")
     return int(n.value)
 
 
 def sparda_compress_keys(shape: SpardaShape, k_cache, t_ctx: int, win_begin: int, win_end: int, k_cmp, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_compress_keys(ctypes.byref(cs), _p(k_cache), t_ctx, win_begin, win_end, _p(k_cmp),
                                        _stream(stream)), "sparda_compress_keys")
 
 
 def sparda_forecast_select(shape: SpardaShape, f, n_q: int, q_pos0: int, k_cmp, sel, cnt, ws=None, ws_bytes: int = 0,
                            stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_forecast_select(ctypes.byref(cs), _p(f), n_q, q_pos0, _p(k_cmp), _p(sel), _p(cnt), _p(ws),
@@ -316,14 +315,14 @@ def sparda_forecast_select(shape: SpardaShape, f, n_q: int, q_pos0: int, k_cmp, 
 
 
 def sparda_forecast_score_max(shape: SpardaShape, f, n_q: int, q_pos0: int, k_cmp, row_max, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_forecast_score_max(ctypes.byref(cs), _p(f), n_q, q_pos0, _p(k_cmp), _p(row_max),
                                             _stream(stream)), "sparda_forecast_score_max")
 
 
 def sparda_multihead_select(shape: SpardaShape, q, n_q: int, q_pos0: int, k_cmp, sm_scale: float, sel, cnt, ws=None,
                             ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_multihead_select(ctypes.byref(cs), _p(q), n_q, q_pos0, _p(k_cmp), float(sm_scale), _p(sel),
@@ -332,7 +331,7 @@ def sparda_multihead_select(shape: SpardaShape, q, n_q: int, q_pos0: int, k_cmp,
 
 def sparda_sparse_attn(shape: SpardaShape, q, n_q: int, q_pos0: int, k, v, kv_mode: int, sel, cnt, sm_scale: float, o,
                        ws=None, ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_sparse_attn(ctypes.byref(cs), _p(q), n_q, q_pos0, _p(k), _p(v), kv_mode, _p(sel), _p(cnt),
@@ -341,7 +340,7 @@ def sparda_sparse_attn(shape: SpardaShape, q, n_q: int, q_pos0: int, k, v, kv_mo
 
 def sparda_decode_step(shape: SpardaShape, f, q_pos: int, k_cmp, q, k, v, sm_scale: float, sel, cnt, o, ws=None,
                        ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_decode_step(ctypes.byref(cs), _p(f), q_pos, _p(k_cmp), _p(q), _p(k), _p(v), float(sm_scale),
@@ -350,7 +349,7 @@ def sparda_decode_step(shape: SpardaShape, f, q_pos: int, k_cmp, q, k, v, sm_sca
 
 def sparda_sparse_attn_noalloc(shape: SpardaShape, q, n_q: int, q_pos0: int, k, v, kv_mode: int, sel, cnt,
                                sm_scale: float, o, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_sparse_attn_noalloc(ctypes.byref(cs), _p(q), n_q, q_pos0, _p(k), _p(v), kv_mode, _p(sel),
                                              _p(cnt), float(sm_scale), _p(o), _stream(stream)),
            "sparda_sparse_attn_noalloc")
@@ -358,27 +357,27 @@ def sparda_sparse_attn_noalloc(shape: SpardaShape, q, n_q: int, q_pos0: int, k, 
 
 def sparda_gather_blocks(shape: SpardaShape, host_k, host_v, sel, cnt, stage_k, stage_v, n_workgroups: int,
                          stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_gather_blocks(ctypes.byref(cs), _p(host_k), _p(host_v), _p(sel), _p(cnt), _p(stage_k),
                                        _p(stage_v), n_workgroups, _stream(stream)), "sparda_gather_blocks")
 
 
 def sparda_stage_append_kv(shape: SpardaShape, k_new, v_new, q_pos: int, sel, cnt, stage_k, stage_v, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_stage_append_kv(ctypes.byref(cs), _p(k_new), _p(v_new), q_pos, _p(sel), _p(cnt), _p(stage_k),
                                          _p(stage_v), _stream(stream)), "sparda_stage_append_kv")
 
 
 def sparda_writeback_kv(shape: SpardaShape, k_new, v_new, n_new: int, pos0: int, host_k, host_v, n_workgroups: int,
                         stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_writeback_kv(ctypes.byref(cs), _p(k_new), _p(v_new), n_new, pos0, _p(host_k), _p(host_v),
                                       n_workgroups, _stream(stream)), "sparda_writeback_kv")
 
 
 def sparda_plan_staging(shape: SpardaShape, sel, cnt, q_pos: int, slot_blk, slot_len, fetch, sel_staged, stage_cnt,
                         n_fetch, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_plan_staging(ctypes.byref(cs), _p(sel), _p(cnt), q_pos, _p(slot_blk), _p(slot_len), _p(fetch),
                                       _p(sel_staged), _p(stage_cnt), _p(n_fetch), _stream(stream)),
            "sparda_plan_staging")
@@ -386,7 +385,7 @@ def sparda_plan_staging(shape: SpardaShape, sel, cnt, q_pos: int, slot_blk, slot
 
 def sparda_indexer_kl(shape: SpardaShape, q, k, f, k_cmp, n_q: int, q_pos0: int, sm_scale: float, k_top: int, loss, d_f,
                       ws=None, ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_indexer_kl(ctypes.byref(cs), _p(q), _p(k), _p(f), _p(k_cmp), n_q, q_pos0, float(sm_scale),
@@ -395,7 +394,7 @@ def sparda_indexer_kl(shape: SpardaShape, q, k, f, k_cmp, n_q: int, q_pos0: int,
 
 def sparda_tree_select(shape: SpardaShape, f, n_nodes: int, t_ctx, t_max: int, parent, k_cmp, sel, cnt, ws=None,
                        ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_tree_select(ctypes.byref(cs), _p(f), n_nodes, _p(t_ctx), t_max, _p(parent), _p(k_cmp), _p(sel),
@@ -404,7 +403,7 @@ def sparda_tree_select(shape: SpardaShape, f, n_nodes: int, t_ctx, t_max: int, p
 
 def sparda_tree_attn(shape: SpardaShape, q, n_nodes: int, t_ctx, t_max: int, parent, k, v, k_tree, v_tree, n_sel: int,
                      sel, cnt, sm_scale: float, o, ws=None, ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_tree_attn(ctypes.byref(cs), _p(q), n_nodes, _p(t_ctx), t_max, _p(parent), _p(k), _p(v),
@@ -414,7 +413,7 @@ def sparda_tree_attn(shape: SpardaShape, q, n_nodes: int, t_ctx, t_max: int, par
 
 def sparda_tree_verify_workspace_size(shape: SpardaShape, n_nodes: int, vocab: int) -> int:
     n = ctypes.c_size_t(0)
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_tree_verify_workspace_size(ctypes.byref(cs), n_nodes, vocab, ctypes.byref(n)),
            "sparda_tree_verify_workspace_size")
     return int(n.value)
@@ -422,7 +421,7 @@ def sparda_tree_verify_workspace_size(shape: SpardaShape, n_nodes: int, vocab: i
 
 def sparda_tree_verify(shape: SpardaShape, n_nodes: int, vocab: int, ld: int, prob_type: int, p, q, tokens, parent, u,
                        path, n_path, next_token, ws=None, ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     _check(load().sparda_tree_verify(ctypes.byref(cs), n_nodes, vocab, ld, prob_type, _p(p), _p(q), _p(tokens),
@@ -447,7 +446,7 @@ def _table(x, n_layers: int):
 
 def sparda_tree_commit(shape: SpardaShape, n_nodes: int, t_ctx, path, n_path, n_layers: int, k_tree, v_tree, k_cache,
                        v_cache, k_cmp, t_new, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     _check(load().sparda_tree_commit(ctypes.byref(cs), n_nodes, _p(t_ctx), _p(path), _p(n_path), n_layers,
                                      _table(k_tree, n_layers), _table(v_tree, n_layers), _table(k_cache, n_layers),
                                      _table(v_cache, n_layers), _table(k_cmp, n_layers), _p(t_new), _stream(stream)),
@@ -477,7 +476,7 @@ def sparda_rotate(rope: SpardaRope, type: int, batch: int, n_heads: int, n_tok: 
 
 def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int, n_new, t_ctx, k_new, v_new, q, q_out, f,
                         f_out, t_new, stream=None):
-    cs, b, h, bf = shape.c(), shape.batch, shape.n_kv_heads, torch.bfloat16
+    cs, b, h, bf = shape._struct(), shape.batch, shape.n_kv_heads, torch.bfloat16
     kv, hq = (b, h, n_max, 128), (b, h * shape.group_size, n_max, 128)
     pages.check(shape)
     _here(rope.freq if rope else None, pages.tensors[0], n_new, t_ctx, k_new, v_new, q, q_out, f, f_out, t_new)
@@ -489,7 +488,7 @@ def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int
 
 def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max: int, sel, cnt, ws=None, ws_bytes: int = 0,
                         stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     pages.check(shape)
@@ -500,7 +499,7 @@ def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max:
 
 def sparda_paged_attn(shape: SpardaShape, pages: SpardaPages, q, t_ctx, t_max: int, sel, cnt, sm_scale: float, o, ws=None,
                       ws_bytes: int = 0, stream=None):
-    cs = shape.c()
+    cs = shape._struct()
     if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
         ws_bytes = ws.numel() * ws.element_size()
     pages.check(shape)

@@ -190,6 +190,19 @@ def test_handles_check_their_tensors():
         sp.sparda_rotate(r, sp.SPARDA_F32, 1, 2, 3, x, pos, 0, x)
 
 
+def test_shape_struct_follows_the_values():
+    """The struct that calls pass on is that of the shape's present values, whatever was done with c()'s."""
+    s = shape(n_kv_heads=2)
+    assert (s._struct().n_kv_heads, s._struct()) == (2, s._struct())
+    s.c().n_kv_heads = 7
+    assert s._struct().n_kv_heads == 2 and s.c() is not s._struct()
+    s.n_kv_heads = 3
+    assert s._struct().n_kv_heads == 3 and s.c().n_kv_heads == 3
+    again = sp.SpardaShape(**s.__dict__)
+    again.batch = 9
+    assert again == shape(n_kv_heads=3, batch=9) and (again._struct().batch, s._struct().batch) == (9, s.batch)
+
+
 def test_frequencies():
     n = 64
     plain = [10000.0 ** (-j / n) for j in range(n)]
