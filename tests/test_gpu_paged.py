@@ -538,6 +538,24 @@ def test_attention_of_interleaved_pools(dev):
     check(got, *ref.attn(q[:, :, 0], k, v, table, t, page, None, None, ref.SCALE))
 
 
+@pytest.mark.parametrize("longest", [300, 1500, 3000])
+def test_attention_of_as_many_sequences_as_fit(dev, longest):
+    """65535 rows, by each division of the work: short contexts on shared pages, one long one, absent ones."""
+    gen, B, page = torch.Generator().manual_seed(longest), 65535, 16
+    n_pages = -(-longest // page) + 7
+    table = torch.randint(n_pages, (B, -(-longest // L) * L // page), generator=gen, dtype=torch.int32)
+    t = torch.randint(-1, 20, (B,), generator=gen, dtype=torch.int32)
+    t[40000], t[-1] = longest, 33
+    k, v = (torch.randn(n_pages, 1, page, D, generator=gen).to(BF) for _ in range(2))
+    q = torch.randn(B, 2, 1, D, generator=gen).to(BF)
+    got = run_attn(dev, shape_of(B, 1, 2, t_cap=longest), sp.SpardaPages(page, table.to(dev), k.to(dev), v.to(dev)), q, t,
+                   longest, None, None)
+    rows = torch.cat([torch.arange(0, B, 977), torch.tensor([39999, 40000, 40001, B - 2, B - 1])])
+    o, w = ref.attn(q[rows, :, 0], k, v, table[rows], t[rows], page, None, None, ref.SCALE)
+    say("worst share of the bar", check(got[rows], o, w))
+    assert not got[t <= 0].any() and torch.isfinite(got).all()
+
+
 def test_attention_nan_and_infinity(dev):
     """A NaN or an infinity in an attended key or value reaches its row, and no other; t_ctx above t_max counts as t_max."""
     gen, rng, page, t = torch.Generator().manual_seed(10), random.Random(10), 64, 700
