@@ -202,6 +202,15 @@ __device__ __forceinline__ void wave_lds_sync() {
   __asm__ __volatile__("" ::: "memory");
 }
 
+// Keeps this wavefront's LDS accesses before it ahead of those behind it, without a wait: the hardware carries out a
+// wavefront's LDS operations in order, so the compiler's order is all that lanes which exchange rows need (fences of
+// wavefront scope are no instructions).
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ uint4 ld16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
 // The same load with the non-temporal hint, for bytes a launch reads exactly once (the decode

@@ -217,6 +217,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, c
         const int z = 4 * x + g;
         *reinterpret_cast<uint4*>(kbuf + z * 256 + 16 * (c ^ (z & 15))) = kr[x];
       }
+      wave_lds_order();  // other lanes' pieces are read
       if constexpr (kMore) load_k(next);
       __builtin_amdgcn_sched_barrier(0);
       f32x4 s[2];
@@ -229,6 +230,7 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, const RowAt& r, c
           s[x] = mfma16x16x32(as_bf16x8(kw), qf[y], s[x]);
         }
       }
+      wave_lds_order();  // before the next unit's stores
       // ---- scores in the exp2 domain; tokens past the limits are replaced, and their V rows too
       const int lim0 = readlane_i(lim, i), lim1 = readlane_i(lim, i + 1);
       float z[8];
@@ -406,7 +408,7 @@ __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, const RowAt& 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   char* mine = kbuf[wave] + c * 512;
-  __builtin_amdgcn_wave_barrier();
+  wave_lds_order();
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
     *reinterpret_cast<f32x4*>(mine + 16 * ((8 * g + 2 * x) ^ (2 * c))) = f32x4{run.acc[0][x], run.acc[1][x], run.acc[2][x], run.acc[3][x]};

@@ -1,0 +1,44 @@
+"""Paged attention on the GPU where every weight is 0 or 1 (paged_counts.py): each token of each unit counts once, with its
+own key, by each division of the work and at any length."""
+import random
+
+import pytest
+import torch
+
+import paged_counts as counts
+from test_gpu_paged import dev, n_bad, run_attn, say, shape_of, table_of  # noqa: F401
+import paper_2606_04511_amd.sparda as sp
+
+pytestmark = pytest.mark.gpu
+
+
+def compare(got, c, H, sel=None, cnt=None):
+    for b in range(len(c.t_ctx)):
+        for h in range(H):
+            want = c.want(b, h, sel, cnt)
+            far = (got[b, h * c.G:(h + 1) * c.G].double() - want).abs() - counts.bar(want)
+            assert (far <= 0).all(), (b, h, int((far > 0).sum()))
+
+
+def case_of(dev, t_ctx, H, G, page, seed, share=0.5, **kw):  # noqa: F811
+    rng, gen = random.Random(seed), torch.Generator().manual_seed(seed)
+    table, n_pages = table_of(rng, len(t_ctx), max(t_ctx), page, lens=t_ctx)
+    c = counts.Counts(gen, table, t_ctx, n_pages, H, G, page, share)
+    shape = shape_of(len(t_ctx), H, G, t_cap=max(t_ctx), **kw)
+    return c, shape, sp.SpardaPages(page, table.to(dev), c.k.to(dev), c.v.to(dev)), rng
+
+
+@pytest.mark.parametrize("case", [
+    # t_ctx, kv heads, heads per group, page, share of the tokens that a head attends
+    ((2048,), 1, 4, 64, 0.5),                                    # units of one wavefront each
+    ((1024,) * 9, 8, 16, 16, 0.02),                              # a few units per wavefront, most of them without a weight
+    ((64, 33, 500) * 100, 2, 3, 32, 0.2),                        # a wavefront per row
+    ((9000,) + (31, 200, 64) * 40, 2, 2, 128, 0.5),              # the line, rows shared by wavefronts and not
+])
+def test_units_meet_their_own_keys(dev, case):  # noqa: F811
+    """A unit's keys pass through LDS that the units before and behind it use too."""
+    t_ctx, H, G, page, share = case
+    say("counts", t_ctx[:4], len(t_ctx), H, G, page)
+    c, shape, pages, _ = case_of(dev, t_ctx, H, G, page, 7, share)
+    t = torch.tensor(t_ctx, dtype=torch.int32)
+    compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), None, None, counts.SCALE), c, H)
