@@ -253,12 +253,54 @@ def _expect(x, name: str, dtype, numel: int):
         raise ValueError(f"{name}: {numel} dense elements of {dtype} expected")
 
 
-def _here(*tensors):
-    """The tensors are in the memory of the current device, whose stream the call goes to."""
-    dev = _device() if torch.cuda.is_initialized() else -2  # (-1: a tensor in host memory)
+def _present() -> int:
+    """The current device, whose stream the calls go to (-2: none in use; a tensor in host memory is on -1)."""
+    return _device() if torch.cuda.is_initialized() else -2
+
+
+def _elsewhere(x, dev: int):
+    raise ValueError(f"a tensor is on {x.device}, the current device is {'cuda:%d' % dev if dev >= 0 else 'not in use'}")
+
+
+def _here(dev: int, *tensors):
+    """The tensors are in the memory of device `dev`."""
     for x in tensors:
         if x is not None and not isinstance(x, (int, tuple)) and x.get_device() != dev:
-            raise ValueError(f"a tensor is on {x.device}, the current device is {'cuda:%d' % dev if dev >= 0 else 'not in use'}")
+            _elsewhere(x, dev)
+
+
+def _dense(x, name: str, dtype, numel: int, dev: int):
+    """The address of a dense tensor of `numel` elements at least on device `dev` (ints and None pass: raw addresses)."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dtype is not dtype or x.numel() < numel or not x.is_contiguous():
+        raise ValueError(f"{name}: {numel} dense elements of {dtype} expected")
+    if x.get_device() != dev:
+        _elsewhere(x, dev)
+    return x.data_ptr()
+
+
+def _expect_pos(pos, batch: int, n_tok: int, pos_ld: int):
+    """Positions [b pos_ld + t], b < batch, t < n_tok, lie in the tensor: a dense one of as many elements, or rows pos_ld apart."""
+    if pos is None or isinstance(pos, int) or batch <= 0 or n_tok <= 0:
+        return
+    if pos.dtype != torch.int32 or not (
+            pos.numel() >= (batch - 1) * pos_ld + n_tok if pos.is_contiguous() else
+            pos.dim() == 2 and pos.shape[0] >= (batch if pos_ld else 1) and pos.shape[1] >= n_tok and
+            (n_tok == 1 or pos.stride(1) == 1) and (batch == 1 or pos_ld == 0 or pos.stride(0) == pos_ld)):
+        raise ValueError(f"pos: int32, {n_tok} dense positions of {batch} sequences {pos_ld} apart expected")
+
+
+def _space(ws, ws_bytes: int, dev: int):
+    """Address and bytes of a workspace (0: all of the tensor)."""
+    if ws is None or isinstance(ws, int):
+        return ws, ws_bytes
+    n = ws.nbytes
+    if ws_bytes > n or not ws.is_contiguous():
+        raise ValueError(f"ws: a dense tensor of {ws_bytes or n} bytes expected")
+    if ws.get_device() != dev:
+        _elsewhere(ws, dev)
+    return ws.data_ptr(), ws_bytes or n
 
 
 _pack_rows = struct.Struct("=Qqqq").pack  # struct sparda_rows
@@ -282,8 +324,11 @@ _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream):
+def _stream(stream, dev: int = -1):
+    """A stream's handle; None: the current one, of device `dev` where the caller has asked for that already."""
     if stream is None:
+        if dev >= 0 and _raw_stream is not None:
+            return _raw_stream(dev)
         if _raw_stream is not None and torch.cuda.is_initialized():
             return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else 0
@@ -469,40 +514,50 @@ def sparda_rope_freqs(rot_dim: int, base: float, scaling: int = SPARDA_ROPE_PLAI
 def sparda_rotate(rope: SpardaRope, type: int, batch: int, n_heads: int, n_tok: int, x, pos, pos_ld: int, y,
                   backward: bool = False, stream=None):
     dtype, size = torch.float32 if type == SPARDA_F32 else torch.bfloat16, (batch, n_heads, n_tok, 128)
-    _here(rope.freq, x, y, pos)
+    dev = _present()
+    _expect_pos(pos, batch, n_tok, pos_ld)
+    _here(dev, rope.freq, x, y, pos)
     _check(load().sparda_rotate(rope.ref, type, batch, n_heads, n_tok, _rows(x, "x", size, dtype), _p(pos),
-                                pos_ld, _rows(y, "y", size, dtype), int(backward), _stream(stream)), "sparda_rotate")
+                                pos_ld, _rows(y, "y", size, dtype), int(backward), _stream(stream, dev)), "sparda_rotate")
 
 
 def sparda_paged_append(shape: SpardaShape, pages: SpardaPages, rope, n_max: int, n_new, t_ctx, k_new, v_new, q, q_out, f,
                         f_out, t_new, stream=None):
-    cs, b, h, bf = shape._struct(), shape.batch, shape.n_kv_heads, torch.bfloat16
-    kv, hq = (b, h, n_max, 128), (b, h * shape.group_size, n_max, 128)
+    cs, b, h, bf, dev = shape._struct(), shape.batch, shape.n_kv_heads, torch.bfloat16, _present()
+    kv, hq, i32 = (b, h, n_max, 128), (b, h * shape.group_size, n_max, 128), torch.int32
     pages.check(shape)
-    _here(rope.freq if rope else None, pages.tensors[0], n_new, t_ctx, k_new, v_new, q, q_out, f, f_out, t_new)
+    n_new, t_ctx, t_new = (_dense(n_new, "n_new", i32, b, dev), _dense(t_ctx, "t_ctx", i32, b, dev),
+                           _dense(t_new, "t_new", i32, b, dev))
+    _here(dev, rope.freq if rope else None, pages.tensors[0], k_new, v_new, q, q_out, f, f_out)
     _check(load().sparda_paged_append(ctypes.byref(cs), pages.ref, rope.ref if rope else None, n_max,
-                                      _p(n_new), _p(t_ctx), _rows(k_new, "k_new", kv, bf), _rows(v_new, "v_new", kv, bf),
+                                      n_new, t_ctx, _rows(k_new, "k_new", kv, bf), _rows(v_new, "v_new", kv, bf),
                                       _rows(q, "q", hq, bf), _rows(q_out, "q_out", hq, bf), _rows(f, "f", kv, bf),
-                                      _rows(f_out, "f_out", kv, bf), _p(t_new), _stream(stream)), "sparda_paged_append")
+                                      _rows(f_out, "f_out", kv, bf), t_new, _stream(stream, dev)), "sparda_paged_append")
 
 
 def sparda_paged_select(shape: SpardaShape, pages: SpardaPages, f, t_ctx, t_max: int, sel, cnt, ws=None, ws_bytes: int = 0,
                         stream=None):
-    cs = shape._struct()
-    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
-        ws_bytes = ws.numel() * ws.element_size()
+    cs, b, rows, dev = shape._struct(), shape.batch, shape.batch * shape.n_kv_heads, _present()
     pages.check(shape)
-    _here(pages.tensors[0], f, t_ctx, sel, cnt, ws)
-    _check(load().sparda_paged_select(ctypes.byref(cs), pages.ref, _p(f), _p(t_ctx), t_max, _p(sel), _p(cnt),
-                                      _p(ws), ws_bytes, _stream(stream)), "sparda_paged_select")
+    _here(dev, pages.tensors[0])
+    space, size = _space(ws, ws_bytes, dev)
+    _check(load().sparda_paged_select(ctypes.byref(cs), pages.ref, _dense(f, "f", torch.bfloat16, rows * 128, dev),
+                                      _dense(t_ctx, "t_ctx", torch.int32, b, dev), t_max,
+                                      _dense(sel, "sel", torch.int16, rows * shape.k_total, dev),
+                                      _dense(cnt, "cnt", torch.int16, rows, dev), space, size, _stream(stream, dev)),
+           "sparda_paged_select")
 
 
 def sparda_paged_attn(shape: SpardaShape, pages: SpardaPages, q, t_ctx, t_max: int, sel, cnt, sm_scale: float, o, ws=None,
                       ws_bytes: int = 0, stream=None):
-    cs = shape._struct()
-    if ws is not None and not isinstance(ws, int) and ws_bytes == 0:
-        ws_bytes = ws.numel() * ws.element_size()
+    cs, b, rows, dev = shape._struct(), shape.batch, shape.batch * shape.n_kv_heads, _present()
+    size = rows * shape.group_size * 128
     pages.check(shape)
-    _here(pages.tensors[0], q, t_ctx, sel, cnt, o, ws)
-    _check(load().sparda_paged_attn(ctypes.byref(cs), pages.ref, _p(q), _p(t_ctx), t_max, _p(sel), _p(cnt),
-                                    float(sm_scale), _p(o), _p(ws), ws_bytes, _stream(stream)), "sparda_paged_attn")
+    _here(dev, pages.tensors[0])
+    space, ws_bytes = _space(ws, ws_bytes, dev)
+    _check(load().sparda_paged_attn(ctypes.byref(cs), pages.ref, _dense(q, "q", torch.bfloat16, size, dev),
+                                    _dense(t_ctx, "t_ctx", torch.int32, b, dev), t_max,
+                                    _dense(sel, "sel", torch.int16, rows * shape.k_total, dev),
+                                    _dense(cnt, "cnt", torch.int16, rows, dev), float(sm_scale),
+                                    _dense(o, "o", torch.bfloat16, size, dev), space, ws_bytes, _stream(stream, dev)),
+           "sparda_paged_attn")
