@@ -98,9 +98,12 @@ inline size_t paged_select_ws(int64_t rows, int64_t t_max, int32_t n_init, int32
 // longest row per workgroup, workgroups per row cost at most 20 us where all other rows are short, and are faster where
 // they are not (us, contexts between half of t and t; line and workgroups per row): 32 rows of t = 500 12.1 and 8.1; 256
 // rows of 1000 24 and 19; 512 rows of 1000 with 4 heads 42 and 35, with 16 heads 55 and 37; 1600 rows of 1000 113 and 101;
-// but 320 rows of 2000 46 and 49, the second round being short.  Rows of the same length need no line: those of one
-// sequence, or of lists that are shorter than the contexts, while they fill at most one round of workgroups (256 rows of 64
-// blocks 85 and 82; 320 rows 107 and 122).
+// but 320 rows of 2000 46 and 49, the second round being short.  The rows of one sequence are of the same length and need no
+// line.  Nor do lists while most contexts are longer than they are, which the host does not know: up to 128 units per
+// workgroup they take none while they fill at most one round of workgroups (256 rows of k blocks; all contexts longer, every
+// second one, one: k = 48 69 and 63, 43 and 40, 20 and 33; k = 64 87 and 84, 53 and 52, 21 and 42; beyond, the line costs
+// little and saves much: k = 96 130 and 129, 77 and 75, 22 and 60; k = 256 337 and 332, 180 and 186, 28 and 146; k = 1000
+// 1270 and 1273, 617 and 701, 58 and 547).
 //
 // Many short rows have a wavefront each, the more units the more rows there are, up to 16 units (a wavefront alone needs 35
 // us for them).  Workgroups per row and a wavefront (us, contexts up to t): 320 rows of t = 60 7.9 and 7.1, of 100 8.3 and
@@ -124,11 +127,12 @@ inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int64_t t_ma
   int64_t s = rows <= kPagedMaxWgs && units > 16 ? kPagedMaxWgs / rows : 1;
   const int64_t most = (units + kPagedWaves - 1) / kPagedWaves;
   s = s < most ? s : most;
-  const bool alike = rows <= kPagedMaxWgs && (batch == 1 || k_total > 0);
+  const bool one_round = rows <= kPagedMaxWgs;
   const int64_t rounds = (rows + kPagedMaxWgs - 1) / kPagedMaxWgs;
   if (units <= (rounds >= 6 ? 16 : rounds >= 4 ? 6 : rounds >= 2 ? 2 : 0))
     return {(int32_t)((rows + kPagedWaves - 1) / kPagedWaves), -1, false};
-  if (alike || units <= 64 * s) return {(int32_t)(rows * s), (int32_t)s, s > 1};
+  if ((one_round && batch == 1) || units <= (one_round && k_total > 0 ? 128 : 64) * s)
+    return {(int32_t)(rows * s), (int32_t)s, s > 1};
   const int64_t wgs = (rows * units + kPagedWaves - 1) / kPagedWaves;
   return {(int32_t)(wgs < kPagedMaxWgs ? wgs : kPagedMaxWgs), 0, true};
 }

@@ -2,10 +2,10 @@
 // context, for sequences of different lengths whose K and V lie in pages (paper Sec. 4.1, Eq. 5).
 //
 // A row is a sequence's KV head with its G query heads; its work is counted in units of 32 tokens.  Where the rows are few
-// and about as long (paged_attn_plan), a row has its own workgroups, which divide it evenly; where they are many and short,
-// a wavefront.  Otherwise the rows lie one behind the other on a line, which is cut into equal pieces, one per wavefront,
-// whatever the lengths are; where a workgroup's piece holds long rows, its wavefronts divide each of them instead.  A
-// wavefront goes over its units once with a running maximum and sum per head; those of a workgroup that share a row join
+// and about as long, or none is long (paged_attn_plan), a row has its own workgroups, which divide it evenly; where they are
+// many and short, a wavefront.  Otherwise the rows lie one behind the other on a line, which is cut into equal pieces, one per
+// wavefront, whatever the lengths are; where a workgroup's piece holds long rows, its wavefronts divide each of them instead.
+// A wavefront goes over its units once with a running maximum and sum per head; those of a workgroup that share a row join
 // their results in LDS.  A row that ends up whole is written; the results of the others go to the workspace and
 // paged_join_kernel joins them.
 //

@@ -42,3 +42,34 @@ def test_units_meet_their_own_keys(dev, case):  # noqa: F811
     c, shape, pages, _ = case_of(dev, t_ctx, H, G, page, 7, share)
     t = torch.tensor(t_ctx, dtype=torch.int32)
     compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), None, None, counts.SCALE), c, H)
+
+
+def lists_of(c, H, k, rng, order):
+    """Sets of up to k blocks: distinct ones in ascending order, or with repeats in any."""
+    sel = torch.full((len(c.t_ctx), H, 1, k), -1, dtype=torch.int16)
+    cnt = torch.zeros(len(c.t_ctx), H, 1, dtype=torch.int16)
+    for b, t in enumerate(c.t_ctx):
+        nb = -(-max(t, 0) // 64)
+        for h in range(H):
+            got = sorted(rng.sample(range(nb), min(nb, k))) if order == "sorted" else [rng.randrange(max(nb, 1)) for _ in range(k)]
+            sel[b, h, 0, :len(got)] = torch.tensor(got, dtype=torch.int16)
+            cnt[b, h, 0] = len(got)
+    return sel, cnt
+
+
+def run_lists(dev, t_ctx, H, G, k, page, order):  # noqa: F811
+    say("lists", t_ctx[:4], len(t_ctx), H, G, k, page, order)
+    c, shape, pages, rng = case_of(dev, t_ctx, H, G, page, k, 0.5, k=k)
+    sel, cnt = lists_of(c, H, k, rng, order)
+    t = torch.tensor(t_ctx, dtype=torch.int32)
+    compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), sel, cnt, counts.SCALE), c, H, sel, cnt)
+
+
+@pytest.mark.parametrize("case", [
+    ((9000,) + tuple(range(0, 620, 20)), 8, 2, 65, 64, "sorted"),       # one list past 128 units per workgroup
+    ((30000, 200, 0, 4000) * 8, 8, 1, 400, 32, "sorted"),                # every fourth list long
+    ((20000,) + (100, 0, 700) * 5, 2, 16, 300, 128, "repeats"),          # workgroups per row, lists of a few blocks many times over
+    ((40000,) + (100, 0, 700) * 21, 2, 4, 300, 128, "sorted"),
+])
+def test_long_lists_among_short_ones(dev, case):  # noqa: F811
+    run_lists(dev, *case)

@@ -1,0 +1,54 @@
+"""How a paged attention call is divided (paged.hpp), computed by the library's own header in a host program."""
+import itertools
+import os
+import subprocess
+
+import pytest
+
+from test_host_sanitizers import CSRC, HIPCC, ROOT, _run
+
+PROGRAM = r'''
+#include <cstdio>
+#include "paged.hpp"
+int main() {
+  long long b, h, g, t, k;
+  while (std::scanf("%lld %lld %lld %lld %lld", &b, &h, &g, &t, &k) == 5) {
+    const sparda::PagedPlan p = sparda::paged_attn_plan((int)b, (int)h, t, (int)k);
+    std::printf("%u %d %d\n", sparda::paged_units(t, (int)k), p.n_wgs, p.n_splits);
+  }
+}
+'''
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    if not os.path.exists(HIPCC):
+        pytest.skip("hipcc not available")
+    d = tmp_path_factory.mktemp("plan")
+    src, exe = str(d / "plan.cpp"), str(d / "plan")
+    with open(src, "w") as fh:
+        fh.write(PROGRAM)
+    _run([HIPCC, "-x", "hip", "--offload-host-only", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC, src, "-o", exe])
+
+    def ask(cases):
+        out = subprocess.run([exe], input="".join("%d %d %d %d %d\n" % c for c in cases), capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, x.split())) for x in out.splitlines()]
+    return ask
+
+
+CASES = list(itertools.product((1, 2, 8, 16, 32, 64, 200, 700), (1, 2, 8), (1, 4, 16), (1, 64, 1000, 8192, 64000, 2097152),
+                               (0, 3, 48, 64, 65, 96, 200, 1000, 32767)))
+
+
+def test_a_long_row_among_short_ones_is_bounded(plan):
+    """Where a row's own workgroups read it and the others may be short, a workgroup has at most 64 units (128 of a list); the
+    rest go to the line."""
+    for (b, h, g, t, k), (units, n_wgs, n_splits) in zip(CASES, plan(CASES)):
+        if n_splits < 0:
+            assert units <= 16 and n_wgs == -(-b * h // 8), (b, h, t, k)
+        elif n_splits > 0:
+            assert n_wgs == b * h * n_splits, (b, h, t, k)
+            if b > 1:
+                assert units <= (128 if k else 64) * n_splits, (b, h, t, k)
+        else:
+            assert 1 <= n_wgs <= 256 and b > 1, (b, h, t, k)
