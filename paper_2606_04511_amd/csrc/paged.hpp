@@ -136,6 +136,18 @@ inline PagedPlan paged_attn_plan(int32_t batch, int32_t n_kv_heads, int64_t t_ma
   const int64_t wgs = (rows * units + kPagedWaves - 1) / kPagedWaves;
   return {(int32_t)(wgs < kPagedMaxWgs ? wgs : kPagedMaxWgs), 0, true};
 }
+// Wavefronts that join a (row, head) pair's results, eight at a time each.  With workgroups per row it has n_splits of them;
+// on the line up to n_wgs / n_kv_heads + 1, since the sequence's other KV heads are as long.  Most rows of a line have few,
+// and a call has `pairs` pairs: wavefronts without results cost more than the rounds that a long row saves (us, one, four and
+// sixteen wavefronts; 64 sequences with a KV head each, one of them of 131072 tokens, the others of 200: 1 head per group 41,
+// 25 and 22, 4 heads 43, 27 and 22, 16 heads 48, 32 and 30; 64 sequences with 4 KV heads of 4 heads 61, 55 and 58; 8 ragged
+// sequences with 8 KV heads 129, 131 and 131; 300 with 8 KV heads of 4 heads, 9600 pairs, 79, 86 and 119; 16000 pairs of
+// one KV head 59, 53 and 107, 64000 60, 107 and 310).
+inline int paged_join_waves(const PagedPlan& p, int32_t n_kv_heads, int64_t pairs) {
+  const int results = p.n_splits > 0 ? p.n_splits : p.n_wgs / n_kv_heads;
+  if (results > 64 && pairs <= 1024) return 16;
+  return results > (p.n_splits > 0 ? 8 : 32) && pairs <= 16384 ? 4 : 1;
+}
 // Two partial results per wavefront, each per head: 128 sums, the maximum and the denominator (4 floats apart).
 constexpr int kPartFloats = 132;
 // Before them a flag per workgroup and the starts of the sequences: 4 bytes each.

@@ -672,11 +672,10 @@ hipError_t launch_paged_attn(const PagedAttnArgs& args, hipStream_t stream) {
     hipLaunchKernelGGL(paged_attn_kernel<false>, grid, block, 0, stream, a, p.n_splits, per);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.joined) return e;
-  // a row has about n_wgs / rows + 1 results: as many wavefronts as take them eight at a time, up to sixteen
-  const int rows = a.batch * a.n_kv_heads, pairs = rows * a.group_size, results = p.n_wgs / rows;
-  if (results > 64)
+  const int pairs = a.batch * a.n_kv_heads * a.group_size, waves = paged_join_waves(p, a.n_kv_heads, pairs);
+  if (waves == 16)
     hipLaunchKernelGGL(paged_join_kernel<16>, dim3((unsigned)pairs), dim3(1024), 0, stream, a, p.n_splits, p.n_wgs, pairs);
-  else if (results > 8)
+  else if (waves == 4)
     hipLaunchKernelGGL(paged_join_kernel<4>, dim3((unsigned)pairs), dim3(256), 0, stream, a, p.n_splits, p.n_wgs, pairs);
   else
     hipLaunchKernelGGL(paged_join_kernel<1>, dim3((unsigned)((pairs + 3) / 4)), dim3(256), 0, stream, a, p.n_splits, p.n_wgs, pairs);

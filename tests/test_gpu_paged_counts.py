@@ -73,3 +73,19 @@ def run_lists(dev, t_ctx, H, G, k, page, order):  # noqa: F811
 ])
 def test_long_lists_among_short_ones(dev, case):  # noqa: F811
     run_lists(dev, *case)
+
+
+@pytest.mark.parametrize("case", [
+    # t_ctx, kv heads, heads per group: the join takes sixteen wavefronts, four, one
+    ((200,) * 30 + (60000,) + (200, 0, -1) * 11, 1, 4),
+    ((30000,) + (200, 0) * 32, 4, 4),
+    ((100, 0) * 32 + (40000, 700), 2, 16),
+    ((50, 0, 64) * 343 + (20000, 1), 1, 16),
+    ((9000, 9000, 8000) * 20, 1, 8),
+])
+def test_one_long_row_on_the_line(dev, case):  # noqa: F811
+    t_ctx, H, G = case
+    say("line", max(t_ctx), len(t_ctx), H, G)
+    c, shape, pages, _ = case_of(dev, t_ctx, H, G, 64, 11)
+    t = torch.tensor(t_ctx, dtype=torch.int32)
+    compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), None, None, counts.SCALE), c, H)
