@@ -210,7 +210,8 @@ hipError_t launch(const PagedSelectArgs& a, hipStream_t stream) {
   // 22.4 and 25.5; 256 rows 26.0 and 29.8.  (32, 16): 1 row of 4K 6.2 and 7.5, of 12K 9.1 and 9.0, of 32K 15.6 and 9.0; 128
   // rows of 64K 33 and 28; 192 rows 37 and 42; 256 rows 46 and 52.
   const bool one = C <= 8192 && (total <= (kBlocks ? 16 : 12) || rows >= 192);
-  if (one || C <= g.n_take) {  // (shorter contexts take every candidate where the longest does)
+  // (shorter contexts take every candidate where the longest does; a budget of the forced blocks alone takes none of any)
+  if (one || C <= g.n_take || g.n_take == 0) {
     const size_t lds = (size_t)(C > 64 ? C : 64) * sizeof(float);
     hipLaunchKernelGGL((paged_row_kernel<kBlocks, true>), dim3((unsigned)rows), dim3(kDecThreads), one ? lds : 256, stream, a, 0);
     return hipGetLastError();

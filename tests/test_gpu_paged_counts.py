@@ -89,3 +89,26 @@ def test_one_long_row_on_the_line(dev, case):  # noqa: F811
     c, shape, pages, _ = case_of(dev, t_ctx, H, G, 64, 11)
     t = torch.tensor(t_ctx, dtype=torch.int32)
     compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), None, None, counts.SCALE), c, H)
+
+
+@pytest.mark.parametrize("grid,page", [((64, 64), 64), ((32, 16), 16)])
+@pytest.mark.parametrize("n_init,n_local", [(1, 2), (0, 1), (4, 32)])
+def test_sets_of_the_forced_blocks_alone(dev, grid, page, n_init, n_local):  # noqa: F811
+    """A budget of the initial and local blocks only: no key is scored, so none is read and the workspace stays as it is."""
+    t_ctx, H, k = (90000, 64 * 40 + 1, 0, 64, 1, 64 * n_local + 1), 2, n_init + n_local
+    say("forced", grid, n_init, n_local)
+    B, t_max = len(t_ctx), max(t_ctx)
+    shape = shape_of(B, H, 1, k, t_max, n_init, n_local, grid)
+    table = torch.zeros(B, -(-shape.t_cap // page), dtype=torch.int32, device=dev)
+    keys = torch.full((1, H, page // grid[1], 128), float("nan"), dtype=counts.BF, device=dev)
+    ws = torch.full((sp.sparda_workspace_size(shape, sp.SPARDA_OP_PAGED_SELECT, 1, t_max - 1),), 0x5A, dtype=torch.uint8, device=dev)
+    sel = torch.full((B, H, 1, k), 77, dtype=torch.int16, device=dev)
+    cnt = torch.full((B, H, 1), 77, dtype=torch.int16, device=dev)
+    sp.sparda_paged_select(shape, sp.SpardaPages(page, table, k_cmp=keys), torch.ones(B, H, 1, 128, dtype=counts.BF, device=dev),
+                           torch.tensor(t_ctx, dtype=torch.int32, device=dev), t_max, sel, cnt, ws)
+    for b, t in enumerate(t_ctx):
+        last = (t - 1) // 64
+        want = sorted(set(range(min(n_init, last + 1))) | set(range(max(0, last - n_local + 1), last + 1))) if t > 0 else []
+        for h in range(H):
+            assert int(cnt[b, h, 0]) == len(want) and sel[b, h, 0].tolist() == want + [-1] * (k - len(want)), (b, h)
+    assert (ws == 0x5A).all()
