@@ -112,3 +112,29 @@ def test_sets_of_the_forced_blocks_alone(dev, grid, page, n_init, n_local):  # n
         for h in range(H):
             assert int(cnt[b, h, 0]) == len(want) and sel[b, h, 0].tolist() == want + [-1] * (k - len(want)), (b, h)
     assert (ws == 0x5A).all()
+
+
+@pytest.mark.parametrize("case", [
+    # t_ctx, kv heads, heads per group, page: the longest contexts and the most units per wavefront
+    ((70000,), 1, 2, 1024),
+    ((33333,), 1, 12, 16),
+    ((100001, 99999), 2, 3, 64),
+    ((20000, 3, 40000, 17) * 3, 2, 8, 256),
+    ((65535, 0, 1, 65537), 1, 1, 65536),
+])
+def test_every_token_of_long_contexts(dev, case):  # noqa: F811
+    t_ctx, H, G, page = case
+    say("long", t_ctx, H, G, page)
+    c, shape, pages, _ = case_of(dev, t_ctx, H, G, page, 5)
+    t = torch.tensor(t_ctx, dtype=torch.int32)
+    compare(run_attn(dev, shape, pages, c.q, t, max(t_ctx), None, None, counts.SCALE), c, H)
+
+
+@pytest.mark.parametrize("case", [
+    ((100000,), 1, 2, 1000, 64, "sorted"),
+    ((100000,), 1, 2, 1000, 16, "repeats"),
+    ((90001,), 2, 16, 1407, 256, "sorted"),          # every block of the context
+    ((40000, 39000), 4, 4, 500, 128, "sorted"),
+])
+def test_every_token_of_long_lists(dev, case):  # noqa: F811
+    run_lists(dev, *case)
