@@ -17,8 +17,8 @@
 // enter the product as two bf16 numbers, which costs matrix time that is free here (they are busy for less than a tenth).
 // The next unit's K and V are under way in registers during a unit's products: 16 KiB per wavefront, 128 KiB per CU.
 //
-// What bounds it: the memory's rate of block reads.  8 sequences of 18K to 33K tokens, 8 KV heads (839 MB): 126 us, 6.7 TB/s,
-// and 4 for the join; 256 rows of 64 blocks (537 MB): 79 us, 6.8 TB/s.  Small calls are chains: length -> page -> K -> V ->
+// What bounds it: the memory's rate of block reads.  8 sequences of 18K to 33K tokens, 8 KV heads (839 MB): 128 us, 6.6 TB/s,
+// and 5 for the join; 256 rows of 64 blocks (537 MB): 81 us, 6.6 TB/s.  Small calls are chains: length -> page -> K -> V ->
 // join in LDS -> second launch, 8.9 us for 8 rows of 4K; a row of a few tokens 4.7.
 #include <type_traits>
 

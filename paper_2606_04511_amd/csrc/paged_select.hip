@@ -5,7 +5,7 @@
 // within the t tokens; a block's score is the largest of the windows that overlap it.  A workgroup per row selects, and
 // forms the scores itself where that is faster (launch has the choice); elsewhere a launch before it does.
 //
-// What bounds it: the memory's rate for many rows (256 rows of 128K: 134 MB in 26 us, of which the top-k is about 5);
+// What bounds it: the memory's rate for many rows (256 rows of 128K: 126 MB in 24 us, of which the top-k is about 5);
 // below, the chain length -> pages -> keys -> top-k, 5.3 us for a row of 4K.
 #include "device_util.hpp"
 #include "launch.hpp"

@@ -1,10 +1,11 @@
 // rotary.hpp -- turning a row of a head by its position (rotate.hip, paged_append.hip).
 //
 // Eight lanes share a row of 128 elements, which they move in pieces of 16 bytes (E elements: 8 of bf16, 4 of float32).
-// A slot is two pieces, A and B, and holds E pairs: lane c has slot c, of float32 rows slot c + 8 too, and an instruction of
-// the eight lanes moves whole runs of 64 bytes at least.  With n pieces in a row, slot q holds pieces q and q + n / 2 where a
-// pair is two neighbours.  Where it lies half the rotated part apart, the slots q < T = rot_dim / (2 E) hold both sides of
-// pairs E q .. E q + E - 1 (pieces q and q + T), the others pieces that pass (q + T and q + n / 2).
+// A slot is two pieces, A and B, and holds E pairs: lane c has slot c, of float32 rows slot c + 8 too.  With n pieces in a
+// row, slot q holds pieces q and q + n / 2 where a pair is two neighbours.  Where it lies half the rotated part apart, the
+// slots q < T = rot_dim / (2 E) hold both sides of pairs E q .. E q + E - 1 (pieces q and q + T), the others pieces that pass
+// (q + T and q + n / 2).  An instruction of the eight lanes moves one run of 128 bytes, or two where the turned slots end
+// among them (halves apart, bf16: runs of rot_dim and 128 - rot_dim bytes).
 //
 // The angle p freq is reduced in float64: at position 131072 a float32 angle is off by up to 2^-7.  Taken in turns,
 // the reduction is a subtraction of the nearest whole number, and the rest, at most half a turn, keeps an
@@ -113,8 +114,9 @@ __device__ __forceinline__ void turn_pieces(const Rope& r, const Slot<4>& t, uin
 }
 
 // Heads that a group of eight lanes walks over, `rows` rows in all: enough that the angles weigh little, while the groups
-// fill the chip (us with 65536 groups, 32768 and 16384: 18 heads of 5300 tokens 15.9, 13.8 and 14; 40 heads of 4000 15.0, 13.5
-// and 15; a prompt's append of 500 tokens in 4 sequences 19.5, 15.5 and 15.8, of 4001 76, 74 and 79).
+// fill the chip (us with 65536 groups, 32768 and 16384, on inputs in turn: 18 heads of 5300 tokens in bf16 14.7, 11.7 and 11.4,
+// in float32 21.6, 20.7 and 21.0; 40 heads of 4000 16.2, 14.8 and 18.1, 34.5, 32.0 and 37.9; an append of 500 tokens in 4
+// sequences 19.1, 16.0 and 15.8, of 4001 86, 87 and 90).
 constexpr int64_t kRotaryGroups = 32768;
 inline int64_t rotary_heads(int64_t rows, int64_t n_heads) {
   int64_t heads = rows / kRotaryGroups;

@@ -3,9 +3,10 @@
 // Eight lanes per row (rotary.hpp); a group of eight lanes forms the angles of a token once and walks over its heads, with
 // the loads of several heads under way.  Rows are read and written once, past the caches.
 //
-// What bounds it: the memory's rate for a copy (32717 tokens of 32 heads: 536 MB in 100 us, 5.4 TB/s; a copy of as much takes
-// 104 us; with ordinary loads and stores it was 114 us), for few rows the launch (2048 float32 rows: 4 us), for rows of one
-// head the angles beside it (a million: 512 MB in 115 us).
+// What bounds it: the memory's rate for a copy (32717 tokens of 32 heads: 536 MB of bf16 in 101 us, 5.3 TB/s, 103 to 105 on
+// inputs in turn; a copy of as much takes 104; with ordinary loads and stores it was 114; 1072 MB of float32 in 210, 5.1
+// TB/s), for few rows the launch (2048 float32 rows: 4 us), for rows of one head the angles beside it (a million of bf16: 516
+// MB in 120 us).
 #include <type_traits>
 
 #include "rotary.hpp"

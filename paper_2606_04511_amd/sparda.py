@@ -122,7 +122,9 @@ class SpardaRope:
 class SpardaPages:
     """The pages of one layer (struct sparda_pages), made once: it holds the tensors and their addresses.
     table: int32 [B][pages of a sequence]; k, v: bf16 [n_pages][Hkv][P][128] (views of one pool with the same stride
-    between pages are fine); k_cmp: bf16 [n_pages][Hkv][P / stride][128], dense.  What a call does not use can be None."""
+    between pages are fine); k_cmp: bf16 [n_pages][Hkv][P / stride][128], dense.  What a call does not use can be None.
+    The calls read the table's memory when they run: a sequence that grows, ends or moves is written into the table in place
+    (one table, and so one handle per layer, for as many sequences and pages as a server has)."""
 
     def __init__(self, page_size: int, table, k=None, v=None, k_cmp=None):
         pools = [x for x in (k, v, k_cmp) if x is not None]
