@@ -5,7 +5,9 @@ import subprocess
 
 import pytest
 
-from test_host_sanitizers import CSRC, HIPCC, ROOT, _run
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2606_04511_amd", "csrc")
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 PROGRAM = r'''
 #include <cstdio>
@@ -28,7 +30,8 @@ def plan(tmp_path_factory):
     src, exe = str(d / "plan.cpp"), str(d / "plan")
     with open(src, "w") as fh:
         fh.write(PROGRAM)
-    _run([HIPCC, "-x", "hip", "--offload-host-only", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC, src, "-o", exe])
+    subprocess.run([HIPCC, "-x", "hip", "--offload-host-only", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+                    src, "-o", exe], check=True)
 
     def ask(cases):
         out = subprocess.run([exe], input="".join("%d %d %d %d %d\n" % c for c in cases), capture_output=True, text=True, check=True).stdout
